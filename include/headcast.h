@@ -271,6 +271,123 @@ int headcast_dense_attend_noalloc(const void* q_dev, const void* k_dev, const vo
 int headcast_noalloc_status(void* stream);
 const char* headcast_noalloc_last_error(void);
 
+/* ---- Rotary positions over time, height and width -------------------------------------------------------
+ * (Not in the paper: what a video transformer does to Q and K before they reach the calls above.)
+ *
+ * A token's row of every head is rotated by its position: pair i of axis a, whose width is D_a, turns by
+ *   phi = scale_a * position_a * theta^(-2 i / D_a),     y0 = x0 cos(phi) - x1 sin(phi),  y1 = x0 sin(phi) + x1 cos(phi).
+ * The pairs of time come first, then height, then width; with halves = 0 pair j of a row is its elements (2j, 2j + 1), with
+ * halves = 1 elements (j, j + R/2), R = dim_t + dim_h + dim_w.  Elements from R on keep their bits.  inverse != 0 turns the other way
+ * (undoing a rotation, or its gradient: the map is orthogonal).  Products in fp32, one rounding to bf16; the angles are
+ * exact for positions of any size. */
+typedef struct headcast_rope_config {
+  int32_t n_heads;          /* heads of q, 1..64 */
+  int32_t n_kv_heads;       /* heads of k, 0..64 (0: no k) */
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t grid_h, grid_w;   /* token grid of one frame; not read where positions are given */
+  int32_t dim_t, dim_h, dim_w; /* rotated width of each axis: even, together 2..head_dim */
+  int32_t halves;           /* pairing, see above; 1 needs dim_t + dim_h + dim_w to be a multiple of 16 */
+  double theta;             /* 10000 */
+  double scale_t, scale_h, scale_w; /* factor on positions (interpolation); 1 */
+} headcast_rope_config;
+
+/* theta 10000, scales 1; sizes are left zero for the caller. */
+void headcast_rope_default_config(headcast_rope_config* cfg);
+
+/* Rotates q_dev [n_tokens][n_heads][d] into q_out_dev and, unless NULL, k_dev [n_tokens][n_kv_heads][d] into k_out_dev (bf16).
+ * q_stride / k_stride: elements between the tokens of an input, 0 for contiguous (a slice of a fused projection has more); a
+ * multiple of 8.  Outputs are contiguous; an output may be its own contiguous input, any other overlap is refused.  Token i is
+ * at (first_frame + i / (grid_h*grid_w), row, column), |first_frame| <= 2^31, or at positions_dev[i] = (time, height, width), int32,
+ * any values.  n_tokens 0 does nothing.  Allocates nothing, keeps nothing, runs on `stream` of the current device and may be
+ * captured.  headcast_rope_last_error: the reason of the calling thread's last failing call. */
+int headcast_rope(const headcast_rope_config* cfg, const void* q_dev, void* q_out_dev, int64_t q_stride, const void* k_dev, void* k_out_dev,
+                  int64_t k_stride, int32_t n_tokens, int64_t first_frame, const int32_t* positions_dev, int32_t inverse, void* stream);
+const char* headcast_rope_last_error(void);
+
+/* ---- A cache held in 4 bits ------------------------------------------------------------------------------
+ * (Not in the paper: for histories that the bf16 caches above have no room for.)
+ *
+ * A packed cache keeps one layer's keys and values in 4 bits per element and 8 bits of scale per 16 elements, 72 instead of 256
+ * bytes per row of 128.  16 neighbouring elements of a row share a scale s, their largest magnitude over 6 rounded to four significant
+ * bits (ties to even) and held within 2^-19 .. 1.875 * 2^12; an element x is held as sign * s * c, c the one of 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 nearest to |x| / s (ties to the even place in this list; more than 6 becomes 6; a NaN becomes 0).  Held values are exact in bf16.
+ * Key/value heads have lengths of their own, which differ after an eviction; query head i reads key/value head
+ * i / (n_heads / n_kv_heads).  Beside its K and V every token has a weight, a float that headcast_packed_observe adds to.
+ *
+ * The caller owns all device memory: the cache's storage, and a workspace per call, which no two calls whose GPU work may overlap
+ * (other streams, graph replays) may share.  Calls allocate nothing and return without waiting (headcast_packed_check
+ * excepted); all but that one may be captured, a replay does what the captured call did: to the lengths that the cache had then.  Calls
+ * that change a cache are ordered by the caller against its others where they are on different streams.  The device on which a
+ * cache was created has to be current.  One cache is used by one host thread at a time. */
+#define HEADCAST_PACKED_MAX_TOKENS 8388608
+typedef struct headcast_packed_config {
+  int32_t n_heads;          /* query heads, 1..64 */
+  int32_t n_kv_heads;       /* key/value heads, a divisor of n_heads */
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t capacity;         /* tokens per head, 1..HEADCAST_PACKED_MAX_TOKENS */
+  float softmax_scale;      /* 0 selects 1/sqrt(d); else 2^-40 .. 2^40 */
+} headcast_packed_config;
+
+typedef struct headcast_packed headcast_packed;
+
+/* Bytes of storage that a cache needs (HC_ERR_INVALID_ARG for a config out of range). */
+int64_t headcast_packed_bytes(const headcast_packed_config* cfg);
+
+/* An empty cache in storage_dev (256-byte aligned, of the current device, kept by the caller until the cache is destroyed and
+ * its work done; contents do not matter).  Clears a status word there in the order of `stream`. */
+int headcast_packed_create(const headcast_packed_config* cfg, void* storage_dev, int64_t storage_bytes, void* stream, headcast_packed** out);
+int headcast_packed_destroy(headcast_packed* cache);
+
+/* Tokens per key/value head, to a HOST array of n_kv_heads. */
+int headcast_packed_lengths(const headcast_packed* cache, int32_t* lengths_host);
+/* Forgets all tokens, or the newest n_tokens of every head (HC_ERR_STATE where a head has fewer): no GPU work. */
+int headcast_packed_clear(headcast_packed* cache);
+int headcast_packed_drop_last(headcast_packed* cache, int32_t n_tokens);
+
+/* Where in the storage the weights are: byte offset of head 0's first; heads are *row_stride floats apart. */
+int64_t headcast_packed_weights_offset(const headcast_packed* cache, int64_t* row_stride);
+
+/* Packs k_dev and v_dev, [n_tokens][n_kv_heads][d] bf16 with tokens token_stride elements apart (0: contiguous; a multiple of 8), behind
+ * every head's last token, with weights of zero.  HC_ERR_STATE, and no change, where a head has no room. */
+int headcast_packed_append(headcast_packed* cache, const void* k_dev, const void* v_dev, int32_t n_tokens, int64_t token_stride, void* stream);
+
+/* The held values of tokens first .. first + n_tokens - 1 as bf16, [n_kv_heads][n_tokens][d]; either output may be NULL.  Rows of
+ * tokens that a head does not have are left as they are. */
+int headcast_packed_export(headcast_packed* cache, int32_t first, int32_t n_tokens, void* k_out_dev, void* v_out_dev, void* stream);
+
+/* Workspace of headcast_packed_attend and headcast_packed_observe with n_queries queries. */
+int64_t headcast_packed_workspace_bytes(const headcast_packed* cache, int32_t n_queries);
+
+/* out[t][i] = softmax(scale * q[t][i] . K) V over all tokens of the key/value head of query head i; q_dev and out_dev
+ * [n_queries][n_heads][d] bf16, contiguous.  lse_dev, unless NULL: [n_heads][n_queries] float, the natural logarithm of the sum of
+ * the exponentials.  A head without tokens gives zeros and -infinity; a query row that holds a NaN or an infinity gives NaN.
+ * Probabilities enter the second product in fp16, sums are fp32.  The result does not depend on anything but the inputs and
+ * the GPU's number of SMs. */
+int headcast_packed_attend(headcast_packed* cache, const void* q_dev, void* out_dev, float* lse_dev, int32_t n_queries, void* workspace_dev,
+                           int64_t workspace_bytes, void* stream);
+
+/* Adds to the weight of every token the attention that it receives from the queries: weight = decay * weight + sum over the rows
+ * of its query heads of exp(scale * q . k - lse), with lse_dev as headcast_packed_attend returned it for the same queries and tokens.
+ * decay: finite, not negative; 1 accumulates, 0 starts anew (whatever the weights held).  n_queries 0 only scales by decay.
+ * Sums are fp32, in an order that depends on sizes alone. */
+int headcast_packed_observe(headcast_packed* cache, const void* q_dev, const float* lse_dev, int32_t n_queries, float decay, void* workspace_dev,
+                            int64_t workspace_bytes, void* stream);
+
+/* Eviction: moves into `to` - whose tokens it replaces - for each key/value head h the min(keep_host[h], length) tokens of cache
+ * that rank highest, with their weights, in their order.  The first n_first and the newest n_recent tokens rank above all
+ * others, those by weight; equal ranks go to the lower place (-0 equals 0, a NaN is below everything).  index_dev, unless NULL:
+ * [n_kv_heads][index_stride] int32, the places that the moved tokens had (entries behind a head's last are left as they
+ * were); without it a workspace of headcast_packed_evict_workspace_bytes() is needed.  `to` is another cache of the same
+ * key/value heads, head_dim and device, in other storage, with room (else HC_ERR_STATE, nothing done).  The source is not changed. */
+int64_t headcast_packed_evict_workspace_bytes(const headcast_packed* cache);
+int headcast_packed_evict(headcast_packed* cache, headcast_packed* to, const int32_t* keep_host, int32_t n_first, int32_t n_recent, int32_t* index_dev,
+                          int32_t index_stride, void* workspace_dev, int64_t workspace_bytes, void* stream);
+
+/* Synchronises `stream` and reports whether a kernel of this cache gave up on a bounded wait (HC_ERR_TIMEOUT; later launches
+ * compute nothing until it is reported). */
+int headcast_packed_check(headcast_packed* cache, void* stream);
+const char* headcast_packed_last_error(const headcast_packed* cache);
+
 #ifdef __cplusplus
 }
 #endif

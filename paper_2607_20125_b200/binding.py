@@ -1,4 +1,4 @@
-"""ctypes binding of libheadcast.so: argument marshalling only.
+"""ctypes binding of libheadcast.so: argument marshalling only (rotary positions and the packed cache: packed.py).
 
 Every method mirrors the C entry point of the same name in include/headcast.h; tensors are torch
 CUDA tensors whose ``data_ptr()`` is handed to the library, and the current torch stream is passed
@@ -24,7 +24,13 @@ EXPORTS = ("headcast_default_config", "headcast_create", "headcast_destroy", "he
            "headcast_set_kernel_timing", "headcast_last_attention_kernel_ms", "headcast_set_tracing",
            "headcast_read_trace", "headcast_dense_attend_noalloc", "headcast_noalloc_status",
            "headcast_noalloc_last_error", "headcast_plan_schedule", "headcast_selftest_bounded_wait", "headcast_overwrite_last",
-           "headcast_append_host", "headcast_attend_host", "headcast_release_memory")
+           "headcast_append_host", "headcast_attend_host", "headcast_release_memory",
+           # bound in packed.py
+           "headcast_rope_default_config", "headcast_rope", "headcast_rope_last_error", "headcast_packed_bytes", "headcast_packed_create",
+           "headcast_packed_destroy", "headcast_packed_lengths", "headcast_packed_clear", "headcast_packed_drop_last",
+           "headcast_packed_weights_offset", "headcast_packed_append", "headcast_packed_export", "headcast_packed_workspace_bytes",
+           "headcast_packed_attend", "headcast_packed_observe", "headcast_packed_evict_workspace_bytes", "headcast_packed_evict",
+           "headcast_packed_check", "headcast_packed_last_error")
 
 
 class Config(C.Structure):

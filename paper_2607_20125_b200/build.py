@@ -6,7 +6,7 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-UNITS = ("headcast_api.cu", "noalloc_scratch.cu")
+UNITS = ("headcast_api.cu", "noalloc_scratch.cu", "packed_api.cu")
 LIB = os.path.join(HERE, "libheadcast.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
@@ -28,7 +28,7 @@ def is_stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles csrc/headcast_api.cu (which includes every kernel header) and csrc/noalloc_scratch.cu into libheadcast.so."""
+    """Compiles the units of csrc (which include the kernel headers) into libheadcast.so."""
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

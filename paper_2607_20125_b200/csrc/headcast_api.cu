@@ -2,30 +2,11 @@
 // tile scheduling, and the launches of the kernels in attn_kernel.cuh / copy_kernels.cuh /
 // score_kernels.cuh.  No CPU fallback exists: every step of the path runs in those kernels.
 #include "context.h"
+#include "launch.h"
 #include "noalloc_scratch.h"
 #include "schedule.h"
 
 namespace {
-
-// Launches a kernel of this library (every one of them calls pdl_wait before it touches global memory, but for lists whose
-// upload was waited for) so that it may become resident while its predecessor on the stream drains.  Since the predecessor may still write while such a kernel
-// runs, nothing is read through the non-coherent path (__ldg, ld.global.nc): that path wants data which no one writes for
-// as long as the reading kernel lives, and pdl_wait orders ordinary loads only.  Together with the one merge launch instead of two it takes
-// the block of 192 tokens and four heads from 86 to 76 us and leaves the large ones where they are (45 x 80: -1 %).
-template <typename... P, typename... A>
-cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = grid;
-  lc.blockDim = block;
-  lc.dynamicSmemBytes = smem;
-  lc.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = &attr;
-  lc.numAttrs = 1;
-  return cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
-}
 
 int upload_schedule(headcast_ctx* c, Schedule& s, cudaStream_t st) {
   // The partial results are shared by all lists of the context, so every launch makes sure of them and not only the first of

@@ -1,0 +1,587 @@
+// Attention of many query rows over a packed cache, on tcgen05 tensor cores.
+//
+// The plan is the one of attn_kernel.cuh - a work item is up to two 128-row query tiles of one key/value head over a range of 128-token
+// tiles; S = Q K^T and O += P V with S, P and O in tensor memory, one thread per query row for the softmax, one issuing
+// warp - with the tile loads replaced by four warps that turn codes into operands:
+//   - a thread owns a token's row: it fetches the row's 64 bytes of codes and 8 of scales (d = 128) one tile ahead, converts them
+//     to fp16 (exact) and writes them into a ring slot in the layout that the products read (128-byte swizzle);
+//   - all operands are fp16: rows of Q are brought to a common power of two first (exact but for elements below 2^-28 of
+//     their row's largest), P keeps 11 bits, so the row sum needs no rounding of its own to match;
+//   - 40 / 72 / 200 / 200 registers for the issuing, converting and the two softmax warpgroups.
+// Rows of a key/value head: row r is token r / group, query head head * group + r % group, so shared heads fill the tiles.
+//
+// The steps (one tile for both query tiles) of all items are laid end to end and every CTA, one per SM, takes an equal share; an
+// item that is cut leaves partial results that packed_merge_kernel joins.  No lists: every role finds its items by division.
+// The packed streams are 3.6 times smaller than bf16, so they share L2 where bf16 streams had to be taken in turn.
+#pragma once
+#include "packed_format.cuh"
+
+namespace hc {
+
+struct PackedAttnParams {
+  PackedView c;
+  const __nv_bfloat16* q;  // [n_queries][n_kv * group][d]
+  __nv_bfloat16* out;
+  float* lse;              // [n_kv * group][n_queries] or null
+  float* part_o;           // [2 * n_cta][256][d] unnormalised; slot 2b: CTA b's first item, which began elsewhere; 2b + 1: its last, which ends elsewhere
+  float2* part_ml;         // [2 * n_cta][256]: reference (log2 domain) and sum
+  int32_t n_queries, group, n_rows, n_pairs;  // n_rows = n_queries * group, n_pairs = ceil(n_rows / 256)
+  int32_t n_cta;
+  float scale_log2e;
+  int64_t line_first[PACK_MAX_HEADS + 1];     // steps of the heads before h: n_pairs times their tiles
+  HeadCounts len;
+};
+
+struct PackedItem {
+  int32_t head, pair, tile_begin, tile_end, tiles, slot;  // slot < 0: the whole range, final
+};
+
+// The item that starts at step x of the line, and ends at `hi` at the latest; x moves behind it.
+__host__ __device__ inline PackedItem packed_item(const PackedAttnParams& p, int cta, int64_t& x, int64_t hi, int& head) {
+  while (p.line_first[head + 1] <= x) ++head;
+  PackedItem w;
+  w.head = head;
+  w.tiles = (p.len.n[head] + PACK_TILE - 1) / PACK_TILE;
+  const int64_t in_head = x - p.line_first[head];
+  w.pair = static_cast<int32_t>(in_head / w.tiles);
+  w.tile_begin = static_cast<int32_t>(in_head - static_cast<int64_t>(w.pair) * w.tiles);
+  const int64_t end = w.tile_begin + (hi - x);
+  w.tile_end = end < w.tiles ? static_cast<int32_t>(end) : w.tiles;
+  x += w.tile_end - w.tile_begin;
+  w.slot = w.tile_begin > 0 ? 2 * cta : w.tile_end < w.tiles ? 2 * cta + 1 : -1;
+  return w;
+}
+
+constexpr int PATTN_THREADS = 512;  // warp 0: MMA, 1-3: idle, 4-7: conversion, 8-11 / 12-15: softmax of query tile 0 / 1
+constexpr int PATTN_REGS_LAUNCH = 128, PATTN_REGS_ISSUE = 40, PATTN_REGS_CONVERT = 72, PATTN_REGS_SOFTMAX = 200;
+static_assert(PATTN_REGS_ISSUE + PATTN_REGS_CONVERT + 2 * PATTN_REGS_SOFTMAX <= 4 * PATTN_REGS_LAUNCH, "the block cannot take more registers than it was launched with");
+constexpr int PATTN_SLOTS = 4;  // ring of K and V tiles, K0 V0 K1 V1 ...
+
+// 2^f on [-1/2, 1/2]: the polynomial of least largest relative error (Lawson's iteration on 4001 Chebyshev points), coefficients rounded to fp32
+constexpr float EX2_C0 = 1.0000001192092896f, EX2_C1 = 0.6931469440460205f, EX2_C2 = 0.24022120237350464f, EX2_C3 = 0.05550713092088699f,
+                EX2_C4 = 0.009675540961325169f, EX2_C5 = 0.0013276472454890609f;
+
+template <int D>
+struct PackedAttnSmem {
+  static constexpr int BLOCK_BYTES = 128 * 128;  // [128 rows][64 fp16], 128-byte swizzle
+  static constexpr int TILE_BYTES = (D / 64) * BLOCK_BYTES;
+  static constexpr int KV_OFF = 2 * TILE_BYTES;
+  static constexpr int DYN_BYTES = KV_OFF + PATTN_SLOTS * TILE_BYTES + 1024;
+};
+
+// 2^x for a packed pair on the FMA pipe: x = n + f with |f| <= 1/2, a polynomial of degree five for 2^f (its relative error, 2e-7, is
+// that of the special-function unit), n added to the exponent.  Inputs at least -126.
+__device__ __forceinline__ void ex2_poly5_pair(uint64_t x2, float& e_lo, float& e_hi) {
+  const uint64_t magic = pack_f32x2(12582912.f, 12582912.f), neg_magic = pack_f32x2(-12582912.f, -12582912.f), neg_one = pack_f32x2(-1.f, -1.f);
+  const uint64_t t2 = add_f32x2(x2, magic);
+  const uint64_t f2 = fma_f32x2(add_f32x2(t2, neg_magic), neg_one, x2);
+  uint64_t p2 = fma_f32x2(f2, pack_f32x2(EX2_C5, EX2_C5), pack_f32x2(EX2_C4, EX2_C4));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(EX2_C3, EX2_C3));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(EX2_C2, EX2_C2));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(EX2_C1, EX2_C1));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(EX2_C0, EX2_C0));
+  float t_lo, t_hi, p_lo, p_hi;
+  unpack_f32x2(t2, t_lo, t_hi);
+  unpack_f32x2(p2, p_lo, p_hi);
+  e_lo = __uint_as_float(__float_as_uint(p_lo) + (__float_as_uint(t_lo) << 23));
+  e_hi = __uint_as_float(__float_as_uint(p_hi) + (__float_as_uint(t_hi) << 23));
+}
+
+template <int D>
+__global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __grid_constant__ PackedAttnParams p) {
+  using SM = PackedAttnSmem<D>;
+  constexpr int QK_STEPS = D / 16;
+  constexpr uint32_t TMEM_COLS = 512;
+  constexpr uint32_t S_COL = 0, O_COL = 256;  // S_t at t*128, O_t at 256 + t*128; P_t overlays the first half of S_t
+  constexpr int P_HEAD = 2;                   // of the four 32-token chunks of P, how many are handed over ahead of the rest
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t bar_q_full[2], bar_s_full[2], bar_p_head[2], bar_p_full[2], bar_o_full[2];
+  __shared__ uint64_t bar_kv_full[PATTN_SLOTS], bar_kv_free[PATTN_SLOTS];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&bar_q_full[t], 4);
+      mbar_init(&bar_s_full[t], 1);
+      mbar_init(&bar_p_head[t], 4);
+      mbar_init(&bar_p_full[t], 4);
+      mbar_init(&bar_o_full[t], 1);
+    }
+    for (int s = 0; s < PATTN_SLOTS; ++s) {
+      mbar_init(&bar_kv_full[s], 4);
+      mbar_init(&bar_kv_free[s], 1);
+    }
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(&tmem_slot, TMEM_COLS);
+    tmem_relinquish();
+  }
+  pdl_launch_dependents();
+  pdl_wait();
+  if (tid == 0) abort_flag = (*reinterpret_cast<volatile int32_t*>(p.c.status) != 0) ? 1 : 0;
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = tmem_slot;
+  volatile int* abortp = &abort_flag;
+  const bool dead_on_arrival = abort_flag != 0;  // a kernel gave up and the host has not heard of it yet
+  __syncthreads();                               // (the flag is read before any wait can raise it)
+  const int64_t total = p.line_first[p.c.n_kv];
+  const int64_t x_lo = share_begin(blockIdx.x, total, p.n_cta), x_hi = share_begin(blockIdx.x + 1, total, p.n_cta);
+  int64_t x = x_lo;
+  int head = 0;
+
+  if (dead_on_arrival) {
+    // nothing: straight to the teardown
+  } else if (warp < 4) {
+    regs_dec<PATTN_REGS_ISSUE>();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- MMA issuer (the whole warp, converged)
+      const uint32_t elected = elect_one();
+      const uint32_t idesc_s = idesc_f16_f32(128, 128, 0, 0), idesc_o = idesc_f16_f32(128, D, 0, 1);
+      const uint32_t q_addr = smem_u32(smem), kv_addr = smem_u32(smem + SM::KV_OFF);
+      const uint64_t q_desc = smem_desc_sw128(q_addr, 16, 1024), k_desc = smem_desc_sw128(kv_addr, 16, 1024);
+      const uint64_t v_desc = smem_desc_sw128(kv_addr, SM::BLOCK_BYTES, 1024);
+      uint32_t kt = 0, q_cnt[2] = {0, 0}, p_cnt[2] = {0, 0};
+      bool ok = true;
+      auto issue_qk = [&](int t, uint32_t st) {
+        mma_block_ss<QK_STEPS>(tmem + S_COL + t * 128, q_desc + ((t * SM::TILE_BYTES) >> 4), k_desc + ((st * SM::TILE_BYTES) >> 4), idesc_s,
+                               SM::BLOCK_BYTES >> 4, elected);
+      };
+      auto wait = [&](uint64_t* bar, uint32_t parity, int code) -> bool { return mbar_wait_warp(bar, parity, abortp, p.c.status, code); };
+      while (ok && x < x_hi) {
+        const PackedItem w = packed_item(p, blockIdx.x, x, x_hi, head);
+        const int nt = w.tile_end - w.tile_begin;
+        const int n_q = w.pair * 256 + 128 < p.n_rows ? 2 : 1;
+        {
+          const uint32_t st = (2 * kt) % PATTN_SLOTS, ph = ((2 * kt) / PATTN_SLOTS) & 1;
+          if (!(ok = wait(&bar_kv_full[st], ph, 71))) break;
+          for (int t = 0; t < n_q && ok; ++t) {
+            if (!(ok = wait(&bar_q_full[t], q_cnt[t] & 1, 72))) break;
+            ++q_cnt[t];
+            tc_fence_after_sync();
+            issue_qk(t, st);
+            mma_commit(&bar_s_full[t], elected);
+          }
+          if (!ok) break;
+          mma_commit(&bar_kv_free[st], elected);
+        }
+        for (int j = 0; j < nt && ok; ++j) {
+          const uint32_t gv = 2 * (kt + j) + 1, gk = gv + 1;  // ring positions of V_j and K_{j+1}
+          const uint32_t st = gv % PATTN_SLOTS, ph = (gv / PATTN_SLOTS) & 1, st1 = gk % PATTN_SLOTS, ph1 = (gk / PATTN_SLOTS) & 1;
+          if (!(ok = wait(&bar_kv_full[st], ph, 73))) break;
+          if (j + 1 < nt && !(ok = wait(&bar_kv_full[st1], ph1, 74))) break;
+          for (int t = 0; t < n_q && ok; ++t) {
+            const uint64_t v_at = v_desc + ((st * SM::TILE_BYTES) >> 4);
+            if (!(ok = wait(&bar_p_head[t], p_cnt[t] & 1, 75))) break;
+            tc_fence_after_sync();
+            mma_block_ts<0, 2 * P_HEAD>(tmem + O_COL + t * 128, tmem + S_COL + t * 128, v_at, idesc_o, j > 0 ? 1u : 0u, elected);
+            if (!(ok = wait(&bar_p_full[t], p_cnt[t] & 1, 76))) break;
+            ++p_cnt[t];
+            tc_fence_after_sync();
+            mma_block_ts<2 * P_HEAD, 8>(tmem + O_COL + t * 128, tmem + S_COL + t * 128, v_at, idesc_o, 1u, elected);
+            if (j + 1 < nt) {
+              issue_qk(t, st1);
+              mma_commit(&bar_s_full[t], elected);
+              if (t == n_q - 1) mma_commit(&bar_kv_free[st1], elected);
+            } else {
+              mma_commit(&bar_o_full[t], elected);
+            }
+          }
+          if (!ok) break;
+          mma_commit(&bar_kv_free[st], elected);
+        }
+        kt += nt;
+      }
+    }
+  } else if (warp < 8) {
+    // ------------------------------------------------------------------ conversion: one thread per token of a tile
+    regs_dec<PATTN_REGS_CONVERT>();
+    constexpr int Q4 = D / 32;  // 16-byte pieces of a row's codes
+    const int row = tid - 128;
+    uint4 codes[Q4];
+    uint32_t scales[D / 64];
+    auto fetch = [&](int h, int tile, bool is_v) {
+      const size_t at = static_cast<size_t>(h) * p.c.cap + static_cast<size_t>(tile) * PACK_TILE + row;
+      const uint4* src = reinterpret_cast<const uint4*>((is_v ? p.c.v_codes : p.c.k_codes) + at * (D / 2));
+#pragma unroll
+      for (int i = 0; i < Q4; ++i) codes[i] = src[i];
+      const uint32_t* sc = reinterpret_cast<const uint32_t*>((is_v ? p.c.v_scales : p.c.k_scales) + at * (D / PACK_GROUP));
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) scales[i] = sc[i];
+    };
+    uint32_t g = 0;
+    bool ok = true;
+    PackedItem w = packed_item(p, blockIdx.x, x, x_hi, head);
+    int tile = w.tile_begin;
+    bool is_v = false, more = true;
+    fetch(w.head, tile, false);
+    while (more) {
+      uint4 now[Q4];
+      uint32_t sc_now[D / 64];
+#pragma unroll
+      for (int i = 0; i < Q4; ++i) now[i] = codes[i];
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) sc_now[i] = scales[i];
+      // the next row is on its way while this one is converted
+      if (!is_v) {
+        is_v = true;
+      } else {
+        is_v = false;
+        if (++tile == w.tile_end) {
+          more = x < x_hi;
+          if (more) {
+            w = packed_item(p, blockIdx.x, x, x_hi, head);
+            tile = w.tile_begin;
+          }
+        }
+      }
+      if (more) fetch(w.head, tile, is_v);
+      const uint32_t st = g % PATTN_SLOTS, ph = (g / PATTN_SLOTS) & 1;
+      ++g;
+      if (!(ok = mbar_wait_warp(&bar_kv_free[st], ph ^ 1, abortp, p.c.status, 77))) break;
+      uint8_t* dst = smem + SM::KV_OFF + st * SM::TILE_BYTES;
+#pragma unroll
+      for (int i = 0; i < Q4; ++i) {
+        const uint32_t words[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int chunk = 4 * i + k;  // eight elements
+          const uint32_t s2 = scale_f16x2(sc_now[chunk / 8], (chunk / 2) % 4);
+          uint32_t v[4];
+          codes_to_f16x2(words[k], v);
+          *reinterpret_cast<uint4*>(dst + (chunk / 8) * SM::BLOCK_BYTES + sw128_offset(row, chunk % 8)) =
+              make_uint4(mul_f16x2(v[0], s2), mul_f16x2(v[1], s2), mul_f16x2(v[2], s2), mul_f16x2(v[3], s2));
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      mbar_arrive_if(&bar_kv_full[st], lane == 0);
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax + epilogue: one thread per query row
+    regs_inc<PATTN_REGS_SOFTMAX>();
+    const int t = (warp - 8) >> 2;
+    const int r = ((warp & 3) << 5) | lane;  // row inside the tile == TMEM lane
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) << 5) << 16;
+    const uint32_t s_addr = tmem + lane_off + S_COL + t * 128, o_addr = tmem + lane_off + O_COL + t * 128;
+    uint8_t* sq = smem + t * SM::TILE_BYTES;
+    const int row0 = r & ~31;
+    const int heads = p.c.n_kv * p.group;
+    uint32_t s_cnt = 0, o_cnt = 0;
+    bool ok = true;
+    while (ok && x < x_hi) {
+      const PackedItem w = packed_item(p, blockIdx.x, x, x_hi, head);
+      const int base = w.pair * 256 + t * 128;  // first row of this tile
+      if (base >= p.n_rows) continue;
+      const bool row_valid = base + r < p.n_rows;
+      // where the row is in q and out, in units of rows
+      int64_t at = 0;
+      if (row_valid) {
+        const int token = (base + r) / p.group;
+        at = static_cast<int64_t>(token) * heads + w.head * p.group + (base + r - token * p.group);
+      }
+      // ---- this warp's 32 query rows, as fp16 relative to a power of two of their own, into shared memory (swizzled); invalid rows are
+      // zero.  CH consecutive lanes share a row.
+      float c = 0.f;  // from logits to the log2 domain
+      {
+        constexpr int CH = D / 8;
+        uint4 v[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+          const int idx = k * 32 + lane, row = idx / CH, ch = idx % CH;
+          const int64_t from = __shfl_sync(0xffffffffu, at, row);
+          const bool valid = __shfl_sync(0xffffffffu, row_valid ? 1 : 0, row) != 0;
+          v[k] = make_uint4(0, 0, 0, 0);
+          if (valid) v[k] = *(reinterpret_cast<const uint4*>(p.q + from * D) + ch);
+        }
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+          const int idx = k * 32 + lane, row = idx / CH, ch = idx % CH;
+          const uint32_t raw[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+          // the largest magnitude as an integer: bf16 magnitudes are ordered like their bits, NaN above infinity
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max(top, max(raw[i] & 0x7fffu, (raw[i] >> 16) & 0x7fffu));
+#pragma unroll
+          for (int o = 1; o < CH; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          float f, back;
+          row_factor(__uint_as_float(top << 16), f, back);
+          const float theirs = __shfl_sync(0xffffffffu, back, (lane % (32 / CH)) * CH);
+          if (lane / (32 / CH) == k) c = p.scale_log2e * theirs;
+          uint32_t y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = pack_f16x2(__uint_as_float(raw[i] << 16) * f, __uint_as_float(raw[i] & 0xffff0000u) * f);
+          *reinterpret_cast<uint4*>(sq + (ch / 8) * SM::BLOCK_BYTES + sw128_offset(row0 + row, ch % 8)) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before_sync();  // orders this thread's TMEM reads of the previous item before the arrive
+        __syncwarp();
+        mbar_arrive_if(&bar_q_full[t], lane == 0);
+      }
+      float m_ref = -INFINITY, l_sum = 0.f;
+      for (int tile = w.tile_begin; tile < w.tile_end; ++tile) {
+        const int n_valid = min(PACK_TILE, p.len.n[w.head] - tile * PACK_TILE);
+        if (!(ok = mbar_wait_warp(&bar_s_full[t], s_cnt & 1, abortp, p.c.status, 78))) break;
+        ++s_cnt;
+        tc_fence_after_sync();
+        uint32_t sv[4][32];
+        float mx;
+        {
+          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_addr + ch * 32, sv[ch]);
+          tmem_wait_ld(sv[0], sv[1], sv[2], sv[3]);
+          if (n_valid < PACK_TILE) {  // the last tile of a head: one branch for the whole tile
+#pragma unroll
+            for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (ch * 32 + i >= n_valid) sv[ch][i] = 0xff800000u;
+          }
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              mx4[0] = max3(mx4[0], __uint_as_float(sv[ch][i]), __uint_as_float(sv[ch][i + 1]));
+              mx4[1] = max3(mx4[1], __uint_as_float(sv[ch][i + 2]), __uint_as_float(sv[ch][i + 3]));
+              mx4[2] = max3(mx4[2], __uint_as_float(sv[ch][i + 4]), __uint_as_float(sv[ch][i + 5]));
+              mx4[3] = max3(mx4[3], __uint_as_float(sv[ch][i + 6]), __uint_as_float(sv[ch][i + 7]));
+            }
+          mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c;
+        }
+        // the reference moves only when some row's maximum outgrows it
+        if (__any_sync(0xffffffffu, mx > m_ref + P_LAG)) {
+          const float m_new = mx > m_ref + P_HEADROOM ? mx - P_HEADROOM : m_ref;
+          const float alpha = (m_new == -INFINITY) ? 1.f : ex2_approx(m_ref - m_new);
+          l_sum *= alpha;
+          m_ref = m_new;
+          if (tile > w.tile_begin) {
+#pragma unroll 1
+            for (int ch = 0; ch < D / 16; ++ch) {
+              uint32_t v[16];
+              tmem_ld16(o_addr + ch * 16, v);
+              tmem_wait_ld(v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+              tmem_st16(o_addr + ch * 16, v);
+            }
+          }
+        }
+        const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
+        const uint64_t c2 = pack_f32x2(c, c), m2 = pack_f32x2(-m_use, -m_use);
+        uint64_t sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(sv[ch][2 * i]), __uint_as_float(sv[ch][2 * i + 1])), c2, m2);
+            float x0, x1, e0, e1;
+            unpack_f32x2(x2, x0, x1);
+            if ((i & 7) == 7) {
+              ex2_poly5_pair(pack_f32x2(fmaxf(x0, -126.f), fmaxf(x1, -126.f)), e0, e1);
+            } else {
+              e0 = ex2_approx(x0);
+              e1 = ex2_approx(x1);
+            }
+            pk[i] = pack_f16x2(e0, e1);
+            sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(e0, e1));
+          }
+          if (ch == P_HEAD) {
+            tmem_wait_st();
+            tc_fence_before_sync();
+            __syncwarp();
+            mbar_arrive_if(&bar_p_head[t], lane == 0);
+          }
+          tmem_st16(s_addr + ch * 16, pk);
+        }
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(&bar_p_full[t], lane == 0);
+        float a0, a1;
+        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a0, a1);
+        l_sum += a0 + a1;
+      }
+      if (!ok) break;
+      // ---- epilogue
+      if (!(ok = mbar_wait_warp(&bar_o_full[t], o_cnt & 1, abortp, p.c.status, 79))) break;
+      ++o_cnt;
+      tc_fence_after_sync();
+      // The warp turns its rows through its own 32 rows of the query buffer, which the last product has finished reading, so that
+      // stores cover whole lines.
+      uint8_t* stg = sq + row0 * 128;
+      if (w.slot < 0) {
+        const float inv = 1.f / l_sum;  // positive, or NaN
+#pragma unroll 1
+        for (int ch = 0; ch < D / 32; ++ch) {
+          uint32_t v[32];
+          tmem_ld32(o_addr + ch * 32, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint4 o4;
+            o4.x = pack_bf16x2(__uint_as_float(v[8 * i + 0]) * inv, __uint_as_float(v[8 * i + 1]) * inv);
+            o4.y = pack_bf16x2(__uint_as_float(v[8 * i + 2]) * inv, __uint_as_float(v[8 * i + 3]) * inv);
+            o4.z = pack_bf16x2(__uint_as_float(v[8 * i + 4]) * inv, __uint_as_float(v[8 * i + 5]) * inv);
+            o4.w = pack_bf16x2(__uint_as_float(v[8 * i + 6]) * inv, __uint_as_float(v[8 * i + 7]) * inv);
+            *reinterpret_cast<uint4*>(stg + (ch >> 1) * SM::BLOCK_BYTES + lane * 128 + ((((ch & 1) * 4 + i) ^ (lane & 7)) << 4)) = o4;
+          }
+        }
+        __syncwarp();
+        constexpr int U = D / 8;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int idx = k * 32 + lane, row = idx / U, u = idx % U;
+          const uint4 val = *reinterpret_cast<const uint4*>(stg + (u / 8) * SM::BLOCK_BYTES + row * 128 + (((u % 8) ^ (row & 7)) << 4));
+          const int64_t to = __shfl_sync(0xffffffffu, at, row);
+          const bool valid = __shfl_sync(0xffffffffu, row_valid ? 1 : 0, row) != 0;
+          if (valid) *reinterpret_cast<uint4*>(p.out + to * D + u * 8) = val;
+        }
+        if (p.lse && row_valid) {
+          const int token = (base + r) / p.group;
+          p.lse[static_cast<size_t>(w.head * p.group + (base + r - token * p.group)) * p.n_queries + token] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+        }
+        __syncwarp();
+      } else {
+        float* dst = p.part_o + (static_cast<size_t>(w.slot) * 256 + t * 128 + row0) * D;
+#pragma unroll 1
+        for (int ch = 0; ch < D / 32; ++ch) {
+          uint32_t v[32];
+          tmem_ld32(o_addr + ch * 32, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<float4*>(stg + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+                make_float4(__uint_as_float(v[4 * i + 0]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int idx = k * 32 + lane, row = idx >> 3, u = idx & 7;
+            const float4 val = *reinterpret_cast<const float4*>(stg + row * 128 + ((u ^ (row & 7)) << 4));
+            const bool valid = __shfl_sync(0xffffffffu, row_valid ? 1 : 0, row) != 0;
+            if (valid) *reinterpret_cast<float4*>(dst + static_cast<size_t>(row) * D + ch * 32 + u * 4) = val;
+          }
+          __syncwarp();
+        }
+        if (row_valid) p.part_ml[static_cast<size_t>(w.slot) * 256 + t * 128 + r] = make_float2(m_ref, l_sum);
+      }
+    }
+  }
+  // ------------------------------------------------------------------ teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// Joins the parts of the query-tile pairs that were cut.  Blocks are dealt by boundary between two shares: the first boundary
+// inside a pair stands for the pair, the others have nothing to do.  A thread takes 8 columns of a row; GROUPS of threads share
+// its parts (1, 4 or 16: the more parts, the more groups), 16 / GROUPS rows per block.
+template <int D, int GROUPS>
+__global__ void __launch_bounds__(16 * D / 8) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
+  constexpr int C = D / 8, ROWS = 16 / GROUPS, BLOCKS = 256 / ROWS;
+  __shared__ float sh_o[16][D];
+  __shared__ float2 sh_ml[16];
+  pdl_launch_dependents();
+  const int boundary = 1 + blockIdx.x / BLOCKS;
+  const int64_t total = p.line_first[p.c.n_kv];
+  const int64_t at = share_begin(boundary, total, p.n_cta);
+  int head = 0;
+  while (p.line_first[head + 1] <= at) ++head;
+  const int tiles = (p.len.n[head] + PACK_TILE - 1) / PACK_TILE;
+  const int pair = static_cast<int>((at - p.line_first[head]) / tiles);
+  const int64_t first = p.line_first[head] + static_cast<int64_t>(pair) * tiles;
+  const int b0 = share_owner(first, total, p.n_cta), n = share_owner(first + tiles - 1, total, p.n_cta) - b0 + 1;
+  const int c = threadIdx.x % C, g = (threadIdx.x / C) % GROUPS, lane_row = threadIdx.x / (C * GROUPS);
+  const int in_pair = (blockIdx.x % BLOCKS) * ROWS + lane_row;
+  const int row = pair * 256 + in_pair;
+  pdl_wait();
+  if (at == first || boundary != b0 + 1 || *reinterpret_cast<volatile int32_t*>(p.c.status) != 0) return;  // the same for the whole block
+  float m = -INFINITY, l = 0.f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (row < p.n_rows) {
+    constexpr int BATCH = 4;  // parts whose loads are all issued before the first is used
+    for (int i0 = g; i0 < n; i0 += BATCH * GROUPS) {
+      float2 ml[BATCH];
+      float4 a[BATCH], b[BATCH];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const int i = min(i0 + k * GROUPS, n - 1);
+        const size_t src = static_cast<size_t>(i == 0 ? 2 * b0 + 1 : 2 * (b0 + i)) * 256 + in_pair;
+        ml[k] = p.part_ml[src];
+        const float4* o = reinterpret_cast<const float4*>(p.part_o + src * D + c * 8);
+        asm volatile("ld.global.cs.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a[k].x), "=f"(a[k].y), "=f"(a[k].z), "=f"(a[k].w) : "l"(o));
+        asm volatile("ld.global.cs.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b[k].x), "=f"(b[k].y), "=f"(b[k].z), "=f"(b[k].w) : "l"(o + 1));
+        if (i0 + k * GROUPS >= n) ml[k].x = -INFINITY;
+      }
+      const float m_new = fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x));
+      const float old = m == -INFINITY ? 0.f : ex2_approx(m - m_new);
+      m = m_new;
+      l *= old;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] *= old;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        if (i0 + k * GROUPS >= n) continue;
+        const float wgt = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - m);  // (a row of NaNs has no maximum: its NaNs count, times zero)
+        l += wgt * ml[k].y;
+        acc[0] += wgt * a[k].x; acc[1] += wgt * a[k].y; acc[2] += wgt * a[k].z; acc[3] += wgt * a[k].w;
+        acc[4] += wgt * b[k].x; acc[5] += wgt * b[k].y; acc[6] += wgt * b[k].z; acc[7] += wgt * b[k].w;
+      }
+    }
+  }
+  if (GROUPS > 1) {
+    const int mine = lane_row * GROUPS + g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sh_o[mine][c * 8 + i] = acc[i];
+    if (c == 0) sh_ml[mine] = make_float2(m, l);
+    __syncthreads();
+    if (g != 0) return;
+    float top = -INFINITY;
+    for (int x = 0; x < GROUPS; ++x) top = fmaxf(top, sh_ml[mine + x].x);
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+    for (int x = 0; x < GROUPS; ++x) {
+      const float wgt = sh_ml[mine + x].x == -INFINITY ? 0.f : ex2_approx(sh_ml[mine + x].x - top);
+      l += wgt * sh_ml[mine + x].y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += wgt * sh_o[mine + x][c * 8 + i];
+    }
+    m = top;
+  }
+  if (row >= p.n_rows) return;
+  const float inv = 1.f / l;
+  const int token = row / p.group, h = head * p.group + (row - token * p.group);
+  uint4 o4;
+  o4.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  o4.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+  o4.z = pack_bf16x2(acc[4] * inv, acc[5] * inv);
+  o4.w = pack_bf16x2(acc[6] * inv, acc[7] * inv);
+  *reinterpret_cast<uint4*>(p.out + (static_cast<size_t>(token) * (p.c.n_kv * p.group) + h) * D + c * 8) = o4;
+  if (p.lse && c == 0) p.lse[static_cast<size_t>(h) * p.n_queries + token] = (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// Rows of heads that hold no token: zeros, and a log-sum-exp of -inf.
+template <int D>
+__global__ void __launch_bounds__(256) packed_empty_kernel(const __grid_constant__ PackedAttnParams p) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int head = blockIdx.y;
+  if (p.len.n[head] != 0) return;
+  const int row = blockIdx.x * (256 / (D / 8)) + threadIdx.x / (D / 8), c = threadIdx.x % (D / 8);
+  if (row >= p.n_rows) return;
+  const int token = row / p.group, h = head * p.group + (row - token * p.group);
+  *reinterpret_cast<uint4*>(p.out + (static_cast<size_t>(token) * (p.c.n_kv * p.group) + h) * D + c * 8) = make_uint4(0, 0, 0, 0);
+  if (p.lse && c == 0) p.lse[static_cast<size_t>(h) * p.n_queries + token] = -INFINITY;
+}
+
+}  // namespace hc

@@ -194,6 +194,11 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(uint32_t m, uint32_t n, ui
          ((m >> 4) << 24);
 }
 
+// The same for fp16 A and B.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(uint32_t m, uint32_t n, uint32_t a_mn_major, uint32_t b_mn_major) {
+  return idesc_bf16_f32(m, n, a_mn_major, b_mn_major) & ~((1u << 7) | (1u << 10));
+}
+
 // Issue blocks.  The products of a whole tile are issued by a CONVERGED warp: every lane walks the same loop and computes
 // the same descriptors, and only the tcgen05.mma itself is predicated on the lane that elect.sync chose.  The
 // descriptors then are warp-uniform values, and the warp keeps up with the tensor pipe whatever else its scheduler runs.
