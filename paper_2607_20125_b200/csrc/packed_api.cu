@@ -28,6 +28,7 @@ struct headcast_packed {
   int device = 0, n_sm = 0;
   float scale = 0.f;
   int32_t len[PACK_MAX_HEADS] = {};
+  unsigned configured = 0;  // kernels whose dynamic shared memory has been set, a bit each
   char error[256] = "";
 };
 
@@ -80,6 +81,16 @@ int enter(headcast_packed* c) {
   return HC_OK;
 }
 
+// The attribute belongs to the function in a CUDA context: every cache sets it once for itself, whatever GPU it is on.
+enum { KERNEL_ROWS = 1, KERNEL_ATTN = 2, KERNEL_OBSERVE = 4, KERNEL_SELECT = 8 };
+template <typename K>
+int allow_smem(headcast_packed* c, unsigned which, K* kernel, int bytes) {
+  if (c->configured & which) return HC_OK;
+  PK_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  c->configured |= which;
+  return HC_OK;
+}
+
 HeadCounts lengths(const headcast_packed* c) {
   HeadCounts n;
   std::memset(&n, 0, sizeof(n));
@@ -128,7 +139,8 @@ int attend_few(headcast_packed* c, const void* q, void* out, float* lse, int32_t
   const int total = step_line(c, p.tile_first, 1);
   p.n_cta = std::min(c->n_sm, total);
   if (total > 0) {
-    PK_CUDA(c, cudaFuncSetAttribute(packed_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsSmem<D>::DYN_BYTES));
+    const int rc = allow_smem(c, KERNEL_ROWS, packed_rows_kernel<D>, RowsSmem<D>::DYN_BYTES);
+    if (rc != HC_OK) return rc;
     PK_CUDA(c, launch_pdl(packed_rows_kernel<D>, dim3(p.n_cta), dim3(ROWS_THREADS), RowsSmem<D>::DYN_BYTES, st, p));
   }
   PK_CUDA(c, launch_pdl(packed_merge_rows_kernel<D>, dim3(p.n_rows, c->cfg.n_kv_heads), dim3(MERGE_GROUPS * D / 4), 0, st, p));
@@ -172,7 +184,8 @@ int attend_many(headcast_packed* c, const void* q, void* out, float* lse, int32_
     if (total > 0) parts = std::max(parts, tiles * p.n_cta / total + 2);
   }
   if (total > 0) {
-    PK_CUDA(c, cudaFuncSetAttribute(packed_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PackedAttnSmem<D>::DYN_BYTES));
+    const int rc = allow_smem(c, KERNEL_ATTN, packed_attn_kernel<D>, PackedAttnSmem<D>::DYN_BYTES);
+    if (rc != HC_OK) return rc;
     PK_CUDA(c, launch_pdl(packed_attn_kernel<D>, dim3(p.n_cta), dim3(PATTN_THREADS), PackedAttnSmem<D>::DYN_BYTES, st, p));
     if (p.n_cta > 1) {
       const int groups = parts <= 4 ? 1 : parts <= 24 ? 4 : 16;
@@ -442,7 +455,7 @@ int headcast_packed_attend(headcast_packed* c, const void* q, void* out, float* 
 
 int headcast_packed_observe(headcast_packed* c, const void* q, const float* lse, int32_t n_queries, float decay, void* workspace, int64_t workspace_bytes,
                             void* stream) {
-  const int rc = enter(c);
+  int rc = enter(c);
   if (rc != HC_OK) return rc;
   if (n_queries < 0 || static_cast<int64_t>(n_queries) * c->cfg.n_heads > INT32_MAX - 512) return fail(c, HC_ERR_INVALID_ARG, "n_queries out of range");
   if (!(decay >= 0.f && std::isfinite(decay))) return fail(c, HC_ERR_INVALID_ARG, "decay must be finite and not negative");
@@ -479,7 +492,8 @@ int headcast_packed_observe(headcast_packed* c, const void* q, const float* lse,
   if (!make_tmap_bf16_2d(&p.q_map, q, row, n_queries, row, 128)) return fail(c, HC_ERR_CUDA, "cuTensorMapEncodeTiled failed or is unavailable");
   const int smem = c->cfg.head_dim == 128 ? ObserveSmem<128>::DYN_BYTES : ObserveSmem<64>::DYN_BYTES;
   auto* kernel = c->cfg.head_dim == 128 ? packed_observe_kernel<128> : packed_observe_kernel<64>;
-  PK_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  rc = allow_smem(c, KERNEL_OBSERVE, kernel, smem);
+  if (rc != HC_OK) return rc;
   PK_CUDA(c, launch_pdl(kernel, dim3(p.n_cta), dim3(POBS_THREADS), smem, st, p));
   if (p.n_cta > 1) PK_CUDA(c, launch_pdl(packed_observe_merge_kernel, dim3(p.n_cta - 1), dim3(256), 0, st, p));
   return HC_OK;
@@ -526,7 +540,8 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     // blocks per head: 4096 tokens each, four a thread, keep a pass over them as short as the barriers around it
     int blocks = 1;
     while (blocks < 8 && blocks * 4096 < longest) blocks *= 2;
-    PK_CUDA(c, cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_SMEM));
+    rc = allow_smem(c, KERNEL_SELECT, evict_select_kernel, SELECT_SMEM);
+    if (rc != HC_OK) return rc;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(blocks * n_kv);
     lc.blockDim = dim3(SELECT_THREADS);

@@ -10,8 +10,12 @@ from __future__ import annotations
 import ctypes as C
 from typing import Optional, Sequence, Union
 
+import torch
+
 from . import binding
-from .binding import HeadCastError, _stream
+from .binding import HeadCastError
+
+_raw_stream = torch._C._cuda_getCurrentRawStream  # torch.cuda.current_stream(device).cuda_stream without making a Stream object
 
 
 class RopeConfig(C.Structure):
@@ -64,35 +68,44 @@ def load_library() -> C.CDLL:
     return lib
 
 
-def _tensor(t, name: str, shape: Sequence[Optional[int]], dtype, contiguous: bool = True) -> int:
-    """Rejects whatever would make a kernel read or write outside the caller's buffer; returns the address."""
-    import torch
+def _refuse(t, name: str, shape, dtype, device: int, contiguous: bool) -> None:
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype must be {dtype}, got {t.dtype}")
-    if t.dim() != len(shape) or any(want is not None and got != want for got, want in zip(t.shape, shape)):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: lives on {t.device}, it has to be on cuda:{device}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must be a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: lives on cuda:{t.device.index}, the current device is cuda:{torch.cuda.current_device()}")
+    raise ValueError(f"{name}: the heads of a token must be contiguous, and tokens must not overlap")
+
+
+def _tensor(t, name: str, shape, dtype, device: int) -> int:
+    """Rejects whatever would make a kernel read or write outside the caller's buffer; returns the address."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous()):
+        _refuse(t, name, shape, dtype, device, True)
     return t.data_ptr()
 
 
-def _rows(t, name: str, shape: Sequence[Optional[int]]):
-    """(address, elements between tokens) of a [tokens, heads, d] bf16 tensor whose tokens may lie apart, as in a slice of a fused projection."""
-    import torch
-    ptr = _tensor(t, name, shape, torch.bfloat16, contiguous=False)
-    n, h, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
-        raise ValueError(f"{name}: the heads of a token must be contiguous")
-    stride = t.stride(0) if n > 1 else h * d
-    if stride < h * d:
-        raise ValueError(f"{name}: tokens must not overlap")
-    return ptr, stride
+def _rows(t, name: str, shape, device: int):
+    """(address, elements between tokens, 0 for contiguous) of a [tokens, heads, d] bf16 tensor whose tokens may lie apart, as in a
+    slice of a fused projection."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device):
+        _refuse(t, name, shape, torch.bfloat16, device, False)
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    n, h, d = shape
+    stride = t.stride(0) if n > 1 else 0
+    if t.stride(2) != 1 or (h > 1 and t.stride(1) != d) or (n > 1 and stride < h * d):
+        _refuse(t, name, shape, torch.bfloat16, device, False)
+    return t.data_ptr(), stride
+
+
+def _count(t) -> int:
+    """Tokens of a [tokens, heads, d] tensor; -1, which no shape matches, for anything else."""
+    return t.shape[0] if isinstance(t, torch.Tensor) and t.dim() == 3 else -1
 
 
 class Rope:
@@ -109,23 +122,23 @@ class Rope:
         cfg.grid_h, cfg.grid_w, cfg.halves, cfg.theta = grid_h, grid_w, int(halves), theta
         cfg.dim_t, cfg.dim_h, cfg.dim_w = dims
         cfg.scale_t, cfg.scale_h, cfg.scale_w = scales
-        self.cfg = cfg
+        self.cfg, self._cfg = cfg, C.byref(cfg)
 
     def apply(self, q, q_out, k=None, k_out=None, first_frame: int = 0, positions=None, inverse: bool = False) -> None:
         """q [n, n_heads, d] into q_out, k [n, n_kv_heads, d] into k_out; outputs contiguous, in place allowed.  positions: int32 [n, 3]."""
-        import torch
-        cfg = self.cfg
+        cfg, n, device = self.cfg, _count(q), torch.cuda.current_device()
         if (k is None) != (k_out is None):
             raise ValueError("k and k_out belong together")
-        q_ptr, q_stride = _rows(q, "q", (None, cfg.n_heads, cfg.head_dim))
-        n = q.shape[0]
-        q_out_ptr = _tensor(q_out, "q_out", (n, cfg.n_heads, cfg.head_dim), torch.bfloat16)
+        shape = (n, cfg.n_heads, cfg.head_dim)
+        q_ptr, q_stride = _rows(q, "q", shape, device)
+        q_out_ptr = _tensor(q_out, "q_out", shape, torch.bfloat16, device)
         k_ptr, k_stride, k_out_ptr = None, 0, None
         if k is not None:
-            k_ptr, k_stride = _rows(k, "k", (n, cfg.n_kv_heads, cfg.head_dim))
-            k_out_ptr = _tensor(k_out, "k_out", (n, cfg.n_kv_heads, cfg.head_dim), torch.bfloat16)
-        pos = None if positions is None else _tensor(positions, "positions", (n, 3), torch.int32)
-        rc = self.lib.headcast_rope(C.byref(cfg), q_ptr, q_out_ptr, q_stride, k_ptr, k_out_ptr, k_stride, n, int(first_frame), pos, int(inverse), _stream())
+            shape = (n, cfg.n_kv_heads, cfg.head_dim)
+            k_ptr, k_stride = _rows(k, "k", shape, device)
+            k_out_ptr = _tensor(k_out, "k_out", shape, torch.bfloat16, device)
+        pos = None if positions is None else _tensor(positions, "positions", (n, 3), torch.int32, device)
+        rc = self.lib.headcast_rope(self._cfg, q_ptr, q_out_ptr, q_stride, k_ptr, k_out_ptr, k_stride, n, first_frame, pos, inverse, _raw_stream(device))
         if rc != 0:
             raise HeadCastError(rc, self.lib.headcast_rope_last_error().decode())
 
@@ -135,7 +148,6 @@ class PackedCache:
     call takes its workspace from torch's allocator on the current stream, so calls and captured graphs share none."""
 
     def __init__(self, n_heads: int, head_dim: int, capacity: int, n_kv_heads: Optional[int] = None, softmax_scale: float = 0.0):
-        import torch
         self._ptr = C.c_void_p()
         self.lib = load_library()
         self.n_heads, self.head_dim, self.capacity = n_heads, head_dim, capacity
@@ -145,8 +157,10 @@ class PackedCache:
         if size < 0:
             raise HeadCastError(size, "sizes out of range (1..64 heads, a divisor of them for keys and values, head_dim 64 or 128, capacity 1..2^23, "
                                       "softmax_scale 0 or 2^-40..2^40)")
-        self.storage = torch.empty(size, dtype=torch.uint8, device="cuda")
-        rc = self.lib.headcast_packed_create(C.byref(self.cfg), self.storage.data_ptr(), size, _stream(), C.byref(self._ptr))
+        self._device = torch.cuda.current_device()
+        self._where = torch.device("cuda", self._device)
+        self.storage = torch.empty(size, dtype=torch.uint8, device=self._where)
+        rc = self.lib.headcast_packed_create(C.byref(self.cfg), self.storage.data_ptr(), size, _raw_stream(self._device), C.byref(self._ptr))
         if rc != 0:
             self._ptr = C.c_void_p()
             raise HeadCastError(rc, "headcast_packed_create failed")
@@ -165,15 +179,11 @@ class PackedCache:
         except Exception:
             pass
 
-    def _check(self, rc: int) -> None:
-        if rc != 0:
-            raise HeadCastError(rc, self.lib.headcast_packed_last_error(self._ptr).decode())
+    def _raise(self, rc: int):
+        raise HeadCastError(rc, self.lib.headcast_packed_last_error(self._ptr).decode())
 
     def _workspace(self, size: int):
-        import torch
-        if size < 0:
-            raise HeadCastError(size, "sizes out of range")
-        return torch.empty(max(int(size), 1), dtype=torch.uint8, device="cuda")
+        return torch.empty(max(size, 0), dtype=torch.uint8, device=self._where)
 
     @property
     def weights(self):
@@ -183,72 +193,95 @@ class PackedCache:
     def lengths(self):
         """Tokens per key/value head."""
         arr = (C.c_int32 * self.n_kv_heads)()
-        self._check(self.lib.headcast_packed_lengths(self._ptr, arr))
+        rc = self.lib.headcast_packed_lengths(self._ptr, arr)
+        if rc != 0:
+            self._raise(rc)
         return list(arr)
 
     def clear(self) -> None:
-        self._check(self.lib.headcast_packed_clear(self._ptr))
+        rc = self.lib.headcast_packed_clear(self._ptr)
+        if rc != 0:
+            self._raise(rc)
 
     def drop_last(self, n_tokens: int) -> None:
-        self._check(self.lib.headcast_packed_drop_last(self._ptr, int(n_tokens)))
+        rc = self.lib.headcast_packed_drop_last(self._ptr, n_tokens)
+        if rc != 0:
+            self._raise(rc)
 
     def append(self, k, v) -> None:
         """k, v [n, n_kv_heads, d] bf16; tokens may lie apart (both alike)."""
-        k_ptr, stride = _rows(k, "k", (None, self.n_kv_heads, self.head_dim))
-        v_ptr, v_stride = _rows(v, "v", (k.shape[0], self.n_kv_heads, self.head_dim))
+        n, device = _count(k), self._device
+        shape = (n, self.n_kv_heads, self.head_dim)
+        k_ptr, stride = _rows(k, "k", shape, device)
+        v_ptr, v_stride = _rows(v, "v", shape, device)
         if stride != v_stride:
-            raise ValueError(f"k and v: tokens must lie equally far apart, got {stride} and {v_stride} elements")
-        self._check(self.lib.headcast_packed_append(self._ptr, k_ptr, v_ptr, k.shape[0], stride, _stream()))
+            raise ValueError(f"k and v: tokens must lie equally far apart, got {k.stride(0)} and {v.stride(0)} elements")
+        rc = self.lib.headcast_packed_append(self._ptr, k_ptr, v_ptr, n, stride, _raw_stream(device))
+        if rc != 0:
+            self._raise(rc)
 
     def export(self, first: int = 0, n_tokens: Optional[int] = None):
         """(K, V) bf16 [n_kv_heads, n, d]: the held values, zeros where a head has no token."""
-        import torch
-        longest, shortest = max(self.lengths()), min(self.lengths())
-        n = max(0, longest - first) if n_tokens is None else n_tokens
+        lengths = self.lengths()
+        n = max(0, max(lengths) - first) if n_tokens is None else n_tokens
         if n < 0:
             raise ValueError(f"n_tokens must not be negative, got {n}")
-        make = torch.empty if first + n <= shortest else torch.zeros
-        k, v = (make((self.n_kv_heads, n, self.head_dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
-        self._check(self.lib.headcast_packed_export(self._ptr, int(first), n, k.data_ptr() if n else None, v.data_ptr() if n else None, _stream()))
+        make = torch.empty if first + n <= min(lengths) else torch.zeros
+        both = make((2, self.n_kv_heads, n, self.head_dim), dtype=torch.bfloat16, device=self._where)
+        k, v = both.unbind(0)
+        rc = self.lib.headcast_packed_export(self._ptr, first, n, k.data_ptr() if n else None, v.data_ptr() if n else None, _raw_stream(self._device))
+        if rc != 0:
+            self._raise(rc)
         return k, v
 
     def attend(self, q, out, lse=None) -> None:
         """q, out [n, n_heads, d] bf16; lse float32 [n_heads, n] or None."""
-        import torch
-        n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else None
-        q_ptr = _tensor(q, "q", (n, self.n_heads, self.head_dim), torch.bfloat16)
-        out_ptr = _tensor(out, "out", (n, self.n_heads, self.head_dim), torch.bfloat16)
-        lse_ptr = None if lse is None else _tensor(lse, "lse", (self.n_heads, n), torch.float32)
-        ws = self._workspace(self.lib.headcast_packed_workspace_bytes(self._ptr, n))
-        self._check(self.lib.headcast_packed_attend(self._ptr, q_ptr, out_ptr, lse_ptr, n, ws.data_ptr(), ws.numel(), _stream()))
+        lib, ptr, n, device = self.lib, self._ptr, _count(q), self._device
+        shape = (n, self.n_heads, self.head_dim)
+        q_ptr = _tensor(q, "q", shape, torch.bfloat16, device)
+        out_ptr = _tensor(out, "out", shape, torch.bfloat16, device)
+        lse_ptr = None if lse is None else _tensor(lse, "lse", (self.n_heads, n), torch.float32, device)
+        size = lib.headcast_packed_workspace_bytes(ptr, n)
+        ws = self._workspace(size)
+        rc = lib.headcast_packed_attend(ptr, q_ptr, out_ptr, lse_ptr, n, ws.data_ptr(), size, _raw_stream(device))
+        if rc != 0:
+            self._raise(rc)
 
     def observe(self, q, lse, decay: float = 1.0) -> None:
         """weights = decay * weights + the attention weight that every token receives from the queries, summed; lse as attend returned it."""
-        import torch
-        n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() == 3 else None
-        q_ptr = _tensor(q, "q", (n, self.n_heads, self.head_dim), torch.bfloat16)
-        lse_ptr = _tensor(lse, "lse", (self.n_heads, n), torch.float32)
-        ws = self._workspace(self.lib.headcast_packed_workspace_bytes(self._ptr, n))
-        self._check(self.lib.headcast_packed_observe(self._ptr, q_ptr, lse_ptr, n, float(decay), ws.data_ptr(), ws.numel(), _stream()))
+        lib, ptr, n, device = self.lib, self._ptr, _count(q), self._device
+        q_ptr = _tensor(q, "q", (n, self.n_heads, self.head_dim), torch.bfloat16, device)
+        lse_ptr = _tensor(lse, "lse", (self.n_heads, n), torch.float32, device)
+        size = lib.headcast_packed_workspace_bytes(ptr, n)
+        ws = self._workspace(size)
+        rc = lib.headcast_packed_observe(ptr, q_ptr, lse_ptr, n, decay, ws.data_ptr(), size, _raw_stream(device))
+        if rc != 0:
+            self._raise(rc)
 
     def evict_into(self, other: "PackedCache", keep: Union[int, Sequence[int]], n_first: int = 0, n_recent: int = 0, index=None) -> None:
         """Moves into ``other`` (its tokens are replaced), per head and in order, the first n_first and newest n_recent tokens and the
         largest weights besides, ``keep`` tokens in all (one number, or one per key/value head; a shorter head moves whole).  index:
         int32 [n_kv_heads, >= longest result] or None, receives the places that the tokens had."""
-        import torch
-        keep = [int(keep)] * self.n_kv_heads if isinstance(keep, int) else [int(v) for v in keep]
-        if len(keep) != self.n_kv_heads:
-            raise ValueError(f"keep: expected {self.n_kv_heads} entries, got {len(keep)}")
+        lib, kv, device = self.lib, self.n_kv_heads, self._device
+        keep = [keep] * kv if isinstance(keep, int) else [int(v) for v in keep]
+        if len(keep) != kv:
+            raise ValueError(f"keep: expected {kv} entries, got {len(keep)}")
         if not isinstance(other, PackedCache) or not other._ptr:
             raise ValueError("other: expected a PackedCache")
-        ptr, width = None, 0
+        ptr, width, ws, size = None, 0, None, 0
         if index is not None:
-            ptr = _tensor(index, "index", (self.n_kv_heads, None), torch.int32)
-            width = index.shape[1]
-        ws = self._workspace(self.lib.headcast_packed_evict_workspace_bytes(self._ptr))
-        self._check(self.lib.headcast_packed_evict(self._ptr, other._ptr, (C.c_int32 * len(keep))(*keep), int(n_first), int(n_recent), ptr, width,
-                                                   ws.data_ptr(), ws.numel(), _stream()))
+            width = index.shape[1] if isinstance(index, torch.Tensor) and index.dim() == 2 else -1
+            ptr = _tensor(index, "index", (kv, width), torch.int32, device)
+        else:
+            size = lib.headcast_packed_evict_workspace_bytes(self._ptr)
+            ws = self._workspace(size)
+        rc = lib.headcast_packed_evict(self._ptr, other._ptr, (C.c_int32 * kv)(*keep), n_first, n_recent, ptr, width, None if ws is None else ws.data_ptr(), size,
+                                       _raw_stream(device))
+        if rc != 0:
+            self._raise(rc)
 
     def check(self) -> None:
         """Synchronises the current stream; raises if a kernel of this cache gave up on a bounded wait."""
-        self._check(self.lib.headcast_packed_check(self._ptr, _stream()))
+        rc = self.lib.headcast_packed_check(self._ptr, _raw_stream(self._device))
+        if rc != 0:
+            self._raise(rc)
