@@ -45,19 +45,22 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// A word of another block's shared memory, at the place where `p` is in this one's.
-__device__ __forceinline__ uint32_t peer_word(const uint32_t* p, uint32_t rank) {
-  uint32_t at, v;
+// Two words of another block's shared memory, at the place where `p` is in this one's.
+__device__ __forceinline__ uint2 peer_words(const uint32_t* p, uint32_t rank) {
+  uint32_t at;
+  uint2 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
   return v;
 }
+constexpr int SELECT_MAX_BLOCKS = 8;  // of a cluster
 
 __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __grid_constant__ SelectParams p) {
   extern __shared__ uint32_t select_smem[];
   uint32_t* const keys = select_smem;
   uint32_t* const hist = select_smem + SELECT_KEYS;  // two histograms, used in turn: one cluster barrier per digit
-  __shared__ uint32_t warp_sum[32], found[2], counts[2], warp_gt[32], warp_eq[32];
+  __shared__ uint32_t warp_sum[32], found[2], warp_gt[32], warp_eq[32];
+  __shared__ alignas(8) uint32_t counts[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank(), ranks = cluster_size();
   const int h = blockIdx.x / ranks;
@@ -86,21 +89,20 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
       const uint32_t key = i < hi ? key_at(i) : 0u;
       const bool counts_in = i < hi && (key & mask) == prefix;
       const uint32_t bin = counts_in ? (key >> shift) & ((1u << bits) - 1u) : 0xffffffffu;
-      // equal weights are common (tokens that nothing has looked at yet): one addition for a warp that agrees
-      int same;
-      __match_all_sync(0xffffffffu, bin, &same);
-      if (same) {
-        if (lane == 0 && counts_in) atomicAdd(&mine[bin], 32u);
-      } else if (counts_in) {
-        atomicAdd(&mine[bin], 1u);
-      }
+      // lanes of one bin add once: weights crowd into few bins, and equal ones (tokens that nothing has looked at yet) into one
+      const uint32_t same = __match_any_sync(0xffffffffu, bin);
+      if (counts_in && lane == __ffs(same) - 1) atomicAdd(&mine[bin], static_cast<uint32_t>(__popc(same)));
     }
     cluster_sync();
     // each thread owns two bins; how many keys lie in higher bins is a suffix sum over threads
     uint32_t c0 = 0, c1 = 0;
-    for (uint32_t x = 0; x < ranks; ++x) {
-      c0 += peer_word(&mine[2 * tid], x);
-      c1 += peer_word(&mine[2 * tid + 1], x);
+    uint2 theirs[SELECT_MAX_BLOCKS];
+#pragma unroll
+    for (uint32_t x = 0; x < SELECT_MAX_BLOCKS; ++x) theirs[x] = x < ranks ? peer_words(&mine[2 * tid], x) : make_uint2(0, 0);
+#pragma unroll
+    for (uint32_t x = 0; x < SELECT_MAX_BLOCKS; ++x) {
+      c0 += theirs[x].x;
+      c1 += theirs[x].y;
     }
     uint32_t suffix = c0 + c1;
 #pragma unroll
@@ -110,8 +112,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
     }
     if (lane == 0) warp_sum[warp] = suffix;
     __syncthreads();
-    uint32_t above = suffix - (c0 + c1);
-    for (int x = warp + 1; x < 32; ++x) above += warp_sum[x];
+    const uint32_t above = suffix - (c0 + c1) + __reduce_add_sync(0xffffffffu, lane > warp ? warp_sum[lane] : 0u);
     if (above < k && k <= above + c0 + c1) {  // exactly one thread
       const bool upper = k <= above + c1;
       found[0] = 2 * tid + (upper ? 1 : 0);
@@ -137,25 +138,22 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
     warp_eq[warp] = n_eq;
   }
   __syncthreads();
-  if (tid == 0) {
-    uint32_t g = 0, e = 0;
-    for (int x = 0; x < 32; ++x) {
-      g += warp_gt[x];
-      e += warp_eq[x];
+  if (warp == 0) {
+    const uint32_t g = __reduce_add_sync(0xffffffffu, warp_gt[lane]), e = __reduce_add_sync(0xffffffffu, warp_eq[lane]);
+    if (lane == 0) {
+      counts[0] = g;
+      counts[1] = e;
     }
-    counts[0] = g;
-    counts[1] = e;
   }
   cluster_sync();
-  uint32_t gt = 0, eq = 0;  // of the tokens before this warp's
-  for (uint32_t x = 0; x < rank; ++x) {
-    gt += peer_word(&counts[0], x);
-    eq += peer_word(&counts[1], x);
+  // of the tokens before this warp's: those of the blocks before, then of the warps before
+  uint2 before_me = make_uint2(0, 0);
+  if (lane < rank) before_me = peer_words(counts, lane);
+  if (lane < warp) {
+    before_me.x += warp_gt[lane];
+    before_me.y += warp_eq[lane];
   }
-  for (int x = 0; x < warp; ++x) {
-    gt += warp_gt[x];
-    eq += warp_eq[x];
-  }
+  uint32_t gt = __reduce_add_sync(0xffffffffu, before_me.x), eq = __reduce_add_sync(0xffffffffu, before_me.y);
   int32_t* out = p.index + static_cast<size_t>(h) * p.index_stride;
   for (int i0 = a; i0 < b; i0 += 32) {
     const int i = i0 + lane;

@@ -82,7 +82,7 @@ int enter(headcast_packed* c) {
 }
 
 // The attribute belongs to the function in a CUDA context: every cache sets it once for itself, whatever GPU it is on.
-enum { KERNEL_ROWS = 1, KERNEL_ATTN = 2, KERNEL_OBSERVE = 4, KERNEL_SELECT = 8 };
+enum { KERNEL_ROWS = 1, KERNEL_ATTN = 2, KERNEL_OBSERVE = 4, KERNEL_SELECT = 8, KERNEL_ROWS_16 = 16 };
 template <typename K>
 int allow_smem(headcast_packed* c, unsigned which, K* kernel, int bytes) {
   if (c->configured & which) return HC_OK;
@@ -139,9 +139,12 @@ int attend_few(headcast_packed* c, const void* q, void* out, float* lse, int32_t
   const int total = step_line(c, p.tile_first, 1);
   p.n_cta = std::min(c->n_sm, total);
   if (total > 0) {
-    const int rc = allow_smem(c, KERNEL_ROWS, packed_rows_kernel<D>, RowsSmem<D>::DYN_BYTES);
+    const bool one = p.n_rows <= 8;
+    const int smem = one ? RowsSmem<D, 1>::DYN_BYTES : RowsSmem<D, 2>::DYN_BYTES;
+    auto* kernel = one ? packed_rows_kernel<D, 1> : packed_rows_kernel<D, 2>;
+    const int rc = allow_smem(c, one ? KERNEL_ROWS : KERNEL_ROWS_16, kernel, smem);
     if (rc != HC_OK) return rc;
-    PK_CUDA(c, launch_pdl(packed_rows_kernel<D>, dim3(p.n_cta), dim3(ROWS_THREADS), RowsSmem<D>::DYN_BYTES, st, p));
+    PK_CUDA(c, launch_pdl(kernel, dim3(p.n_cta), dim3(rows_threads(one ? 1 : 2)), smem, st, p));
   }
   PK_CUDA(c, launch_pdl(packed_merge_rows_kernel<D>, dim3(p.n_rows, c->cfg.n_kv_heads), dim3(MERGE_GROUPS * D / 4), 0, st, p));
   return HC_OK;
@@ -188,9 +191,12 @@ int attend_many(headcast_packed* c, const void* q, void* out, float* lse, int32_
     if (rc != HC_OK) return rc;
     PK_CUDA(c, launch_pdl(packed_attn_kernel<D>, dim3(p.n_cta), dim3(PATTN_THREADS), PackedAttnSmem<D>::DYN_BYTES, st, p));
     if (p.n_cta > 1) {
+      int64_t pairs = 0;
+      for (int h = 0; h < c->cfg.n_kv_heads; ++h) pairs += c->len[h] > 0 ? p.n_pairs : 0;
+      const bool by_pair = pairs < p.n_cta - 1;
       const int groups = parts <= 4 ? 1 : parts <= 24 ? 4 : 16;
       auto* merge = groups == 1 ? packed_merge_kernel<D, 1> : groups == 4 ? packed_merge_kernel<D, 4> : packed_merge_kernel<D, 16>;
-      PK_CUDA(c, launch_pdl(merge, dim3((p.n_cta - 1) * 16 * groups), dim3(16 * D / 8), 0, st, p));
+      PK_CUDA(c, launch_pdl(merge, dim3((by_pair ? static_cast<int>(pairs) : p.n_cta - 1) * 16 * groups), dim3(16 * D / 8), 0, st, p, by_pair));
     }
   }
   if (empty) {
@@ -282,14 +288,17 @@ int headcast_rope(const headcast_rope_config* cfg, const void* q, void* q_out, i
   const int dims[3] = {cfg->dim_t, cfg->dim_h, cfg->dim_w};
   const double scales[3] = {cfg->scale_t, cfg->scale_h, cfg->scale_w};
   for (int a = 0, i = 0; a < 3; ++a)
-    for (int j = 0; j < dims[a] / 2; ++j, ++i) {
-      // whole turns per position change nothing
-      const long double turns = static_cast<long double>(scales[a]) * powl(static_cast<long double>(cfg->theta), -2.0L * j / dims[a]) / 6.283185307179586476925286766559L;
+  {
+    // One power per axis: 31 products in 64 bits of mantissa lose 2^-59, and a power takes 100 ns, of which 64 were half of a small call.
+    const long double ratio = dims[a] ? powl(static_cast<long double>(cfg->theta), -2.0L / dims[a]) : 1.0L;
+    long double turns = static_cast<long double>(scales[a]) / 6.283185307179586476925286766559L;
+    for (int j = 0; j < dims[a] / 2; ++j, ++i, turns *= ratio) {
       if (!std::isfinite(static_cast<double>(turns))) return rope_fail(HC_ERR_INVALID_ARG, "a frequency is not finite");
-      const long double fraction = turns - floorl(turns);
+      const long double fraction = turns - floorl(turns);  // whole turns per position change nothing
       uint64_t f = fraction >= 1.0L - 0x1p-64L ? 0 : static_cast<uint64_t>(fraction * 0x1p64L);
       p.frequency[i] = inverse ? 0 - f : f;
     }
+  }
   // tokens of a block: as many as leave every SM a few blocks, at most 8 (their sines and cosines are formed once for all heads)
   int per_block = 8;
   while (per_block > 1 && (n_tokens + per_block - 1) / per_block < 148 * 4) per_block /= 2;
@@ -405,7 +414,7 @@ int headcast_packed_append(headcast_packed* c, const void* k, const void* v, int
   p.stride = stride;
   p.n = n_tokens;
   p.first = lengths(c);
-  const int rows = PACK_THREADS / (c->cfg.head_dim / PACK_GROUP);
+  const int rows = pack_block_tokens(c->cfg.head_dim);
   PK_CUDA(c, launch_pdl(c->cfg.head_dim == 128 ? pack_rows_kernel<128> : pack_rows_kernel<64>, dim3((n_tokens + rows - 1) / rows, c->cfg.n_kv_heads, 2),
                         dim3(PACK_THREADS), 0, static_cast<cudaStream_t>(stream), p));
   for (int h = 0; h < c->cfg.n_kv_heads; ++h) c->len[h] += n_tokens;
@@ -426,7 +435,7 @@ int headcast_packed_export(headcast_packed* c, int32_t first, int32_t n_tokens, 
   p.n = n_tokens;
   p.first = first;
   p.len = lengths(c);
-  const int rows = PACK_THREADS / (c->cfg.head_dim / PACK_GROUP);
+  const int rows = pack_block_tokens(c->cfg.head_dim);
   PK_CUDA(c, launch_pdl(c->cfg.head_dim == 128 ? unpack_rows_kernel<128> : unpack_rows_kernel<64>, dim3((n_tokens + rows - 1) / rows, c->cfg.n_kv_heads, 2),
                         dim3(PACK_THREADS), 0, static_cast<cudaStream_t>(stream), p));
   return HC_OK;
@@ -539,7 +548,7 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     s.n_recent = n_recent;
     // blocks per head: 4096 tokens each, four a thread, keep a pass over them as short as the barriers around it
     int blocks = 1;
-    while (blocks < 8 && blocks * 4096 < longest) blocks *= 2;
+    while (blocks < SELECT_MAX_BLOCKS && blocks * 4096 < longest) blocks *= 2;
     rc = allow_smem(c, KERNEL_SELECT, evict_select_kernel, SELECT_SMEM);
     if (rc != HC_OK) return rc;
     cudaLaunchConfig_t lc = {};

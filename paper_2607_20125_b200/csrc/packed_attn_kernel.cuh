@@ -3,11 +3,12 @@
 // The plan is the one of attn_kernel.cuh - a work item is up to two 128-row query tiles of one key/value head over a range of 128-token
 // tiles; S = Q K^T and O += P V with S, P and O in tensor memory, one thread per query row for the softmax, one issuing
 // warp - with the tile loads replaced by four warps that turn codes into operands:
-//   - a thread owns a token's row: it fetches the row's 64 bytes of codes and 8 of scales (d = 128) one tile ahead, converts them
-//     to fp16 (exact) and writes them into a ring slot in the layout that the products read (128-byte swizzle);
+//   - codes and scales arrive in shared memory by bulk copies, up to three tiles ahead; the warps convert them to fp16 (exact) and
+//     write them into a ring slot in the layout that the products read (128-byte swizzle).  (Fetched into registers instead, a tile
+//     took 1600 clk to convert: the fence behind its stores also waits for the loads that are under way for the next.);
 //   - all operands are fp16: rows of Q are brought to a common power of two first (exact but for elements below 2^-28 of
 //     their row's largest), P keeps 11 bits, so the row sum needs no rounding of its own to match;
-//   - 40 / 72 / 200 / 200 registers for the issuing, converting and the two softmax warpgroups.
+//   - 56 / 72 / 192 / 192 registers for the issuing, converting and the two softmax warpgroups.
 // Rows of a key/value head: row r is token r / group, query head head * group + r % group, so shared heads fill the tiles.
 //
 // The steps (one tile for both query tiles) of all items are laid end to end and every CTA, one per SM, takes an equal share; an
@@ -52,21 +53,24 @@ __host__ __device__ inline PackedItem packed_item(const PackedAttnParams& p, int
   return w;
 }
 
-constexpr int PATTN_THREADS = 512;  // warp 0: MMA, 1-3: idle, 4-7: conversion, 8-11 / 12-15: softmax of query tile 0 / 1
-constexpr int PATTN_REGS_LAUNCH = 128, PATTN_REGS_ISSUE = 40, PATTN_REGS_CONVERT = 72, PATTN_REGS_SOFTMAX = 200;
+constexpr int PATTN_THREADS = 512;  // warp 0: MMA, 1: loads, 2-3: idle, 4-7: conversion, 8-11 / 12-15: softmax of query tile 0 / 1
+constexpr int PATTN_REGS_LAUNCH = 128, PATTN_REGS_ISSUE = 56, PATTN_REGS_CONVERT = 72, PATTN_REGS_SOFTMAX = 192;
 static_assert(PATTN_REGS_ISSUE + PATTN_REGS_CONVERT + 2 * PATTN_REGS_SOFTMAX <= 4 * PATTN_REGS_LAUNCH, "the block cannot take more registers than it was launched with");
-constexpr int PATTN_SLOTS = 4;  // ring of K and V tiles, K0 V0 K1 V1 ...
+constexpr int PATTN_SLOTS = 4;       // ring of converted K and V tiles, K0 V0 K1 V1 ...
+constexpr int PATTN_CODE_SLOTS = 3;  // and of their codes on the way in
 
-// 2^f on [-1/2, 1/2]: the polynomial of least largest relative error (Lawson's iteration on 4001 Chebyshev points), coefficients rounded to fp32
-constexpr float EX2_C0 = 1.0000001192092896f, EX2_C1 = 0.6931469440460205f, EX2_C2 = 0.24022120237350464f, EX2_C3 = 0.05550713092088699f,
-                EX2_C4 = 0.009675540961325169f, EX2_C5 = 0.0013276472454890609f;
+// 2^f on [-1/2, 1/2]: of the polynomials with value 1 at 0 (whole powers come out exact, 2^128 as infinity) the one of least largest
+// relative error (Lawson's iteration on 4001 Chebyshev points), coefficients rounded to fp32
+constexpr float EX2_C0 = 1.f, EX2_C1 = 0.693147004f, EX2_C2 = 0.240222424f, EX2_C3 = 0.0555073358f, EX2_C4 = 0.00967151299f, EX2_C5 = 0.00132647273f;
 
 template <int D>
 struct PackedAttnSmem {
   static constexpr int BLOCK_BYTES = 128 * 128;  // [128 rows][64 fp16], 128-byte swizzle
   static constexpr int TILE_BYTES = (D / 64) * BLOCK_BYTES;
   static constexpr int KV_OFF = 2 * TILE_BYTES;
-  static constexpr int DYN_BYTES = KV_OFF + PATTN_SLOTS * TILE_BYTES + 1024;
+  static constexpr int CODE_OFF = KV_OFF + PATTN_SLOTS * TILE_BYTES;
+  static constexpr int CODE_BYTES = PACK_TILE * (D / 2 + D / PACK_GROUP);  // codes, then scales
+  static constexpr int DYN_BYTES = CODE_OFF + PATTN_CODE_SLOTS * CODE_BYTES + 1024;
 };
 
 // 2^x for a packed pair on the FMA pipe: x = n + f with |f| <= 1/2, a polynomial of degree five for 2^f (its relative error, 2e-7, is
@@ -98,7 +102,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t bar_q_full[2], bar_s_full[2], bar_p_head[2], bar_p_full[2], bar_o_full[2];
-  __shared__ uint64_t bar_kv_full[PATTN_SLOTS], bar_kv_free[PATTN_SLOTS];
+  __shared__ uint64_t bar_kv_full[PATTN_SLOTS], bar_kv_free[PATTN_SLOTS], bar_c_full[PATTN_CODE_SLOTS], bar_c_free[PATTN_CODE_SLOTS];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
@@ -110,6 +114,10 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
       mbar_init(&bar_p_head[t], 4);
       mbar_init(&bar_p_full[t], 4);
       mbar_init(&bar_o_full[t], 1);
+    }
+    for (int s = 0; s < PATTN_CODE_SLOTS; ++s) {
+      mbar_init(&bar_c_full[s], 1);
+      mbar_init(&bar_c_free[s], 4);
     }
     for (int s = 0; s < PATTN_SLOTS; ++s) {
       mbar_init(&bar_kv_full[s], 4);
@@ -198,70 +206,79 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         }
         kt += nt;
       }
+    } else if (warp == 1 && lane == 0) {
+      // ---------------------------------------------------------------- codes and scales of K and V tiles, in the order of their use
+      uint32_t g = 0;
+      bool ok = true;
+      while (ok && x < x_hi) {
+        const PackedItem w = packed_item(p, blockIdx.x, x, x_hi, head);
+        size_t row = static_cast<size_t>(w.head) * p.c.cap + static_cast<size_t>(w.tile_begin) * PACK_TILE;
+        for (int tile = w.tile_begin; tile < w.tile_end && ok; ++tile, row += PACK_TILE)
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t cs = g % PATTN_CODE_SLOTS;
+            if (!(ok = mbar_wait(&bar_c_free[cs], ((g / PATTN_CODE_SLOTS) & 1) ^ 1, abortp, p.c.status, 81))) break;
+            uint8_t* dst = smem + SM::CODE_OFF + cs * SM::CODE_BYTES;
+            mbar_arrive_expect_tx(&bar_c_full[cs], SM::CODE_BYTES);
+            bulk_load(dst, (kv ? p.c.v_codes : p.c.k_codes) + row * (D / 2), PACK_TILE * D / 2, &bar_c_full[cs]);
+            bulk_load(dst + PACK_TILE * D / 2, (kv ? p.c.v_scales : p.c.k_scales) + row * (D / PACK_GROUP), PACK_TILE * D / PACK_GROUP, &bar_c_full[cs]);
+            ++g;
+          }
+      }
+      if (!ok) {  // the copies in flight land before the block leaves
+        for (uint32_t back = 1; back <= PATTN_CODE_SLOTS && back <= g; ++back) {
+          int local_abort = 0;
+          mbar_wait(&bar_c_full[(g - back) % PATTN_CODE_SLOTS], ((g - back) / PATTN_CODE_SLOTS) & 1, &local_abort, p.c.status, 82);
+        }
+      }
     }
   } else if (warp < 8) {
-    // ------------------------------------------------------------------ conversion: one thread per token of a tile
+    // ------------------------------------------------------------------ conversion
     regs_dec<PATTN_REGS_CONVERT>();
-    constexpr int Q4 = D / 32;  // 16-byte pieces of a row's codes
-    const int row = tid - 128;
-    uint4 codes[Q4];
-    uint32_t scales[D / 64];
-    auto fetch = [&](int h, int tile, bool is_v) {
-      const size_t at = static_cast<size_t>(h) * p.c.cap + static_cast<size_t>(tile) * PACK_TILE + row;
-      const uint4* src = reinterpret_cast<const uint4*>((is_v ? p.c.v_codes : p.c.k_codes) + at * (D / 2));
-#pragma unroll
-      for (int i = 0; i < Q4; ++i) codes[i] = src[i];
-      const uint32_t* sc = reinterpret_cast<const uint32_t*>((is_v ? p.c.v_scales : p.c.k_scales) + at * (D / PACK_GROUP));
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) scales[i] = sc[i];
-    };
+    // D / 32 lanes share a row, 16 bytes of codes each; a warp converts its 32 rows in passes.  The upper half of them takes
+    // its words in another order: both halves then write to different banks (they hold the same columns of different 64-column blocks).
+    constexpr int PARTS = D / 32, ROWS = 32 / PARTS, PASSES = 32 / ROWS;
+    const int part = lane % PARTS;
+    const bool swap = PARTS == 4 && part >= 2;
     uint32_t g = 0;
     bool ok = true;
-    PackedItem w = packed_item(p, blockIdx.x, x, x_hi, head);
-    int tile = w.tile_begin;
-    bool is_v = false, more = true;
-    fetch(w.head, tile, false);
-    while (more) {
-      uint4 now[Q4];
-      uint32_t sc_now[D / 64];
+    while (ok && x < x_hi) {
+      const PackedItem w = packed_item(p, blockIdx.x, x, x_hi, head);
+      const uint32_t end = g + 2 * (w.tile_end - w.tile_begin);
+      for (; g != end; ++g) {
+        const uint32_t cs = g % PATTN_CODE_SLOTS, st = g % PATTN_SLOTS;
+        if (!(ok = mbar_wait_warp(&bar_c_full[cs], (g / PATTN_CODE_SLOTS) & 1, abortp, p.c.status, 77))) break;
+        const uint8_t* codes = smem + SM::CODE_OFF + cs * SM::CODE_BYTES;
+        uint4 c[PASSES];
+        uint32_t sc[PASSES];
 #pragma unroll
-      for (int i = 0; i < Q4; ++i) now[i] = codes[i];
+        for (int i = 0; i < PASSES; ++i) {
+          const int row = (warp & 3) * 32 + i * ROWS + lane / PARTS;
+          c[i] = *reinterpret_cast<const uint4*>(codes + row * (D / 2) + part * 16);
+          sc[i] = *reinterpret_cast<const uint16_t*>(codes + PACK_TILE * D / 2 + row * (D / PACK_GROUP) + part * 2);
+        }
+        if (!(ok = mbar_wait_warp(&bar_kv_free[st], ((g / PATTN_SLOTS) & 1) ^ 1, abortp, p.c.status, 80))) break;
+        uint8_t* dst = smem + SM::KV_OFF + st * SM::TILE_BYTES + (part / 2) * SM::BLOCK_BYTES;
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) sc_now[i] = scales[i];
-      // the next row is on its way while this one is converted
-      if (!is_v) {
-        is_v = true;
-      } else {
-        is_v = false;
-        if (++tile == w.tile_end) {
-          more = x < x_hi;
-          if (more) {
-            w = packed_item(p, blockIdx.x, x, x_hi, head);
-            tile = w.tile_begin;
+        for (int i = 0; i < PASSES; ++i) {
+          const int row = (warp & 3) * 32 + i * ROWS + lane / PARTS;
+          const uint32_t words[4] = {swap ? c[i].z : c[i].x, swap ? c[i].w : c[i].y, swap ? c[i].x : c[i].z, swap ? c[i].y : c[i].w};
+          const uint32_t s_lo = scale_f16x2(sc[i], 0), s_hi = scale_f16x2(sc[i], 1);
+          const uint32_t s2[2] = {swap ? s_hi : s_lo, swap ? s_lo : s_hi};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int chunk = (part & 1) * 4 + (k ^ (swap ? 2 : 0));  // eight elements
+            uint32_t v[4];
+            codes_to_f16x2(words[k], v);
+            *reinterpret_cast<uint4*>(dst + sw128_offset(row, chunk)) =
+                make_uint4(mul_f16x2(v[0], s2[k / 2]), mul_f16x2(v[1], s2[k / 2]), mul_f16x2(v[2], s2[k / 2]), mul_f16x2(v[3], s2[k / 2]));
           }
         }
+        fence_proxy_async_smem();
+        __syncwarp();
+        mbar_arrive_if(&bar_kv_full[st], lane == 0);
+        // Only now, when every loaded word has been used: an arrival right behind the loads let the next copy in before they were done.
+        mbar_arrive_if(&bar_c_free[cs], lane == 0);
       }
-      if (more) fetch(w.head, tile, is_v);
-      const uint32_t st = g % PATTN_SLOTS, ph = (g / PATTN_SLOTS) & 1;
-      ++g;
-      if (!(ok = mbar_wait_warp(&bar_kv_free[st], ph ^ 1, abortp, p.c.status, 77))) break;
-      uint8_t* dst = smem + SM::KV_OFF + st * SM::TILE_BYTES;
-#pragma unroll
-      for (int i = 0; i < Q4; ++i) {
-        const uint32_t words[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int chunk = 4 * i + k;  // eight elements
-          const uint32_t s2 = scale_f16x2(sc_now[chunk / 8], (chunk / 2) % 4);
-          uint32_t v[4];
-          codes_to_f16x2(words[k], v);
-          *reinterpret_cast<uint4*>(dst + (chunk / 8) * SM::BLOCK_BYTES + sw128_offset(row, chunk % 8)) =
-              make_uint4(mul_f16x2(v[0], s2), mul_f16x2(v[1], s2), mul_f16x2(v[2], s2), mul_f16x2(v[3], s2));
-        }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      mbar_arrive_if(&bar_kv_full[st], lane == 0);
     }
   } else {
     // ------------------------------------------------------------------ softmax + epilogue: one thread per query row
@@ -483,29 +500,35 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
   }
 }
 
-// Joins the parts of the query-tile pairs that were cut.  Blocks are dealt by boundary between two shares: the first boundary
-// inside a pair stands for the pair, the others have nothing to do.  A thread takes 8 columns of a row; GROUPS of threads share
+// Joins the parts of the query-tile pairs that were cut.  Blocks are dealt by pair (by_pair: of the heads that hold tokens), or, where
+// those are fewer, by boundary between two shares: the first boundary inside a pair stands for the pair, the others have nothing to do.  A thread takes 8 columns of a row; GROUPS of threads share
 // its parts (1, 4 or 16: the more parts, the more groups), 16 / GROUPS rows per block.
 template <int D, int GROUPS>
-__global__ void __launch_bounds__(16 * D / 8) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
+__global__ void __launch_bounds__(16 * D / 8) packed_merge_kernel(const __grid_constant__ PackedAttnParams p, bool by_pair) {
   constexpr int C = D / 8, ROWS = 16 / GROUPS, BLOCKS = 256 / ROWS;
   __shared__ float sh_o[16][D];
   __shared__ float2 sh_ml[16];
   pdl_launch_dependents();
-  const int boundary = 1 + blockIdx.x / BLOCKS;
+  const int index = blockIdx.x / BLOCKS;
   const int64_t total = p.line_first[p.c.n_kv];
-  const int64_t at = share_begin(boundary, total, p.n_cta);
-  int head = 0;
-  while (p.line_first[head + 1] <= at) ++head;
+  int head = 0, pair = 0;
+  if (by_pair) {
+    int left = index / p.n_pairs;  // heads with tokens before it
+    while (p.len.n[head] == 0 || left-- > 0) ++head;
+    pair = index % p.n_pairs;
+  } else {
+    const int64_t at = share_begin(index + 1, total, p.n_cta);
+    while (p.line_first[head + 1] <= at) ++head;
+    pair = static_cast<int>((at - p.line_first[head]) / ((p.len.n[head] + PACK_TILE - 1) / PACK_TILE));
+  }
   const int tiles = (p.len.n[head] + PACK_TILE - 1) / PACK_TILE;
-  const int pair = static_cast<int>((at - p.line_first[head]) / tiles);
   const int64_t first = p.line_first[head] + static_cast<int64_t>(pair) * tiles;
   const int b0 = share_owner(first, total, p.n_cta), n = share_owner(first + tiles - 1, total, p.n_cta) - b0 + 1;
   const int c = threadIdx.x % C, g = (threadIdx.x / C) % GROUPS, lane_row = threadIdx.x / (C * GROUPS);
   const int in_pair = (blockIdx.x % BLOCKS) * ROWS + lane_row;
   const int row = pair * 256 + in_pair;
   pdl_wait();
-  if (at == first || boundary != b0 + 1 || *reinterpret_cast<volatile int32_t*>(p.c.status) != 0) return;  // the same for the whole block
+  if (n < 2 || (!by_pair && index != b0) || *reinterpret_cast<volatile int32_t*>(p.c.status) != 0) return;  // the same for the whole block
   float m = -INFINITY, l = 0.f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (row < p.n_rows) {
     constexpr int BATCH = 4;  // parts whose loads are all issued before the first is used

@@ -4,10 +4,10 @@
 
 namespace hc {
 
-// One thread packs one group of 16 elements: it reads 32 bytes and writes 8 bytes of codes and a scale byte.  d/16 neighbouring
-// threads share a row, a block takes PACK_ROWS(d) consecutive tokens of one head, so that the rows it writes are one contiguous
-// range (64 B of codes per row at d = 128), while its reads are whole rows of 2d bytes, a token apart.  Bound by memory at
-// block sizes: 2 bytes read and 0.56 written per element, once each.
+// A thread takes eight elements: 16 bytes of bf16, 4 of codes; two neighbours share a scale.  D / 8 threads share a row and a block takes
+// PACK_UNROLL times PACK_THREADS * 8 / D consecutive tokens of one head: the rows it writes are one contiguous range of
+// codes, and every load and store of a warp covers whole 32-byte sectors (with 16 elements per thread, two 16-byte accesses half a
+// sector each, unpacking a 45 x 80 block took 20 us instead of UNPACK_US).  Both kernels are bound by memory at block sizes.
 struct PackParams {
   PackedView c;
   const __nv_bfloat16* k;  // [n][n_kv][d], rows of tokens `stride` elements apart
@@ -16,34 +16,52 @@ struct PackParams {
   int32_t n;
   HeadCounts first;        // the slot of the first new token, per head
 };
-constexpr int PACK_THREADS = 256;
+constexpr int PACK_THREADS = 256, PACK_UNROLL = 4;
+__host__ __device__ constexpr int pack_block_tokens(int d) { return PACK_UNROLL * PACK_THREADS * 8 / d; }
 
 template <int D>
 __global__ void __launch_bounds__(PACK_THREADS) pack_rows_kernel(const __grid_constant__ PackParams p) {
-  constexpr int G = D / PACK_GROUP;
+  constexpr int U = D / 8, STEP = PACK_THREADS / U;
   pdl_launch_dependents();
   pdl_wait();
   const int h = blockIdx.y;
   const bool is_v = blockIdx.z != 0;
-  const int g = threadIdx.x % G;
-  const int token = blockIdx.x * (PACK_THREADS / G) + threadIdx.x / G;
-  if (token >= p.n) return;
-  const uint4* src = reinterpret_cast<const uint4*>((is_v ? p.v : p.k) + static_cast<size_t>(token) * p.stride + static_cast<size_t>(h) * D) + 2 * g;
-  const uint4 q[2] = {src[0], src[1]};
-  const uint32_t raw[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
-  float x[PACK_GROUP];
+  const int u = threadIdx.x % U;
+  const int token0 = blockIdx.x * pack_block_tokens(D) + threadIdx.x / U;
+  const __nv_bfloat16* src = (is_v ? p.v : p.k) + static_cast<size_t>(h) * D + 8 * u;
+  uint4 raw[PACK_UNROLL];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float lo = __uint_as_float(raw[i] << 16), hi = __uint_as_float(raw[i] & 0xffff0000u);
-    x[2 * i] = lo != lo ? 0.f : lo;
-    x[2 * i + 1] = hi != hi ? 0.f : hi;
+  for (int i = 0; i < PACK_UNROLL; ++i) {
+    const int token = token0 + i * STEP;
+    raw[i] = make_uint4(0, 0, 0, 0);
+    if (token < p.n) raw[i] = *reinterpret_cast<const uint4*>(src + static_cast<size_t>(token) * p.stride);
   }
-  uint32_t codes[2];
-  const uint32_t scale = pack_group(x, codes);
-  const size_t row = static_cast<size_t>(h) * p.c.cap + p.first.n[h] + token;
-  reinterpret_cast<uint2*>(is_v ? p.c.v_codes : p.c.k_codes)[row * G + g] = make_uint2(codes[0], codes[1]);
-  (is_v ? p.c.v_scales : p.c.k_scales)[row * G + g] = static_cast<uint8_t>(scale);
-  if (!is_v && g == 0) p.c.weights[row] = 0.f;
+#pragma unroll
+  for (int i = 0; i < PACK_UNROLL; ++i) {
+    uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+    // magnitudes of bf16 are ordered like their bits, a NaN above infinity
+    auto largest = [&]() {
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = __vmaxu2(top, w[k] & 0x7fff7fffu);
+      return max(top & 0xffffu, top >> 16);
+    };
+    uint32_t top = largest();
+    if (top > 0x7f80u) {  // a NaN counts as zero
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] &= __vcmpleu2(w[k] & 0x7fff7fffu, 0x7f807f80u);
+      top = largest();
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const uint32_t scale = scale_byte(__uint_as_float(top << 16));
+    const uint32_t word = pack_word(w, scale);
+    const int token = token0 + i * STEP;
+    if (token >= p.n) continue;
+    const size_t row = static_cast<size_t>(h) * p.c.cap + p.first.n[h] + token;
+    reinterpret_cast<uint32_t*>(is_v ? p.c.v_codes : p.c.k_codes)[row * U + u] = word;
+    if (!(u & 1)) (is_v ? p.c.v_scales : p.c.k_scales)[row * (U / 2) + u / 2] = static_cast<uint8_t>(scale);
+    if (!is_v && u == 1) p.c.weights[row] = 0.f;
+  }
 }
 
 // The held values as bf16, [n_kv][n][d]: rows of tokens that a head does not have are left as they are.
@@ -58,24 +76,35 @@ struct UnpackParams {
 
 template <int D>
 __global__ void __launch_bounds__(PACK_THREADS) unpack_rows_kernel(const __grid_constant__ UnpackParams p) {
-  constexpr int G = D / PACK_GROUP;
+  constexpr int U = D / 8, STEP = PACK_THREADS / U;
   pdl_launch_dependents();
   pdl_wait();
   const int h = blockIdx.y;
   const bool is_v = blockIdx.z != 0;
   __nv_bfloat16* out = is_v ? p.v : p.k;
-  const int g = threadIdx.x % G;
-  const int token = blockIdx.x * (PACK_THREADS / G) + threadIdx.x / G;
-  if (!out || token >= p.n || p.first + token >= p.len.n[h]) return;
-  const size_t row = static_cast<size_t>(h) * p.c.cap + p.first + token;
-  const uint2 w = reinterpret_cast<const uint2*>(is_v ? p.c.v_codes : p.c.k_codes)[row * G + g];
-  const float s = scale_value((is_v ? p.c.v_scales : p.c.k_scales)[row * G + g], 0);
-  uint32_t a[4], b[4];
-  word_to_bf16x2(w.x, s, a);
-  word_to_bf16x2(w.y, s, b);
-  uint4* dst = reinterpret_cast<uint4*>(out + (static_cast<size_t>(h) * p.n + token) * D) + 2 * g;
-  dst[0] = make_uint4(a[0], a[1], a[2], a[3]);
-  dst[1] = make_uint4(b[0], b[1], b[2], b[3]);
+  if (!out) return;
+  const int u = threadIdx.x % U;
+  const int token0 = blockIdx.x * pack_block_tokens(D) + threadIdx.x / U, n = min(p.n, p.len.n[h] - p.first);
+  const size_t row0 = static_cast<size_t>(h) * p.c.cap + p.first;
+  const uint32_t* codes = reinterpret_cast<const uint32_t*>(is_v ? p.c.v_codes : p.c.k_codes);
+  const uint8_t* scales = is_v ? p.c.v_scales : p.c.k_scales;
+  uint32_t w[PACK_UNROLL], s[PACK_UNROLL];
+#pragma unroll
+  for (int i = 0; i < PACK_UNROLL; ++i) {
+    const int token = token0 + i * STEP;
+    if (token < n) {
+      w[i] = codes[(row0 + token) * U + u];
+      s[i] = scales[(row0 + token) * (U / 2) + u / 2];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PACK_UNROLL; ++i) {
+    const int token = token0 + i * STEP;
+    if (token >= n) continue;
+    uint32_t v[4];
+    word_to_bf16x2(w[i], scale_value(s[i], 0), v);
+    *reinterpret_cast<uint4*>(out + (static_cast<size_t>(h) * p.n + token) * D + 8 * u) = make_uint4(v[0], v[1], v[2], v[3]);
+  }
 }
 
 }  // namespace hc

@@ -2,12 +2,13 @@
 // exp(scale * q_i . k_j - lse_i), with the log-sum-exps that the attention returned.
 //
 // Only logits are needed, and sums over queries: so the product is turned around, S^T = K Q^T, tokens on the 128 lanes of tensor
-// memory and queries in its columns.  A thread then owns a token and adds up its columns in registers.  A work item is a pair of
+// memory and queries in its columns.  Two threads own a token and add up half its columns each in registers.  A work item is a pair of
 // token tiles (256 tokens) of one key/value head, converted to bf16 (exact) once and kept in shared memory, over a range of
 // query tiles that arrive by TMA as the caller left them.  Items are laid end to end and cut into equal shares like
 // those of packed_attn_kernel; sums of cut items are joined in the order of the line, so results do not vary from run to run.
 //   warp 0 issues products, warp 1 loads query tiles, warps 2 and 3 their log-sum-exps, warps 4-7 convert the next pair of
-//   tiles while this one is in use, warps 8-11 / 12-15 take tile 0 / 1.
+//   tiles while this one is in use, warps 8-23 add up: four per scheduler, since with two (a thread per token) the loop waited for its own
+//   latencies, 3300 clk a step.
 // What bounds it: one exponential per logit, 2 * 128 * 128 per step, 2048 clk of the special-function unit beside 1024 clk of
 // products; a quarter of the exponentials is therefore evaluated on the FMA pipe.
 #pragma once
@@ -15,8 +16,10 @@
 
 namespace hc {
 
-constexpr int POBS_THREADS = 512;
+constexpr int POBS_THREADS = 768;
 constexpr int POBS_LSE_SLOTS = 4;
+constexpr int POBS_POLY_MASK = 1;  // every other group of four columns has two of them take the polynomial
+constexpr float WEIGHS_NOTHING = -1e30f;
 
 struct PackedObserveParams {
   PackedView c;
@@ -68,13 +71,14 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
       bar_s_full[2], bar_s_free[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
+  __shared__ float other_half[256];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bar_k_full[i], 4);
       mbar_init(&bar_k_free[i], 1);
       mbar_init(&bar_s_full[i], 1);
-      mbar_init(&bar_s_free[i], 8);
+      mbar_init(&bar_s_free[i], 16);
     }
     for (int i = 0; i < SM::Q_SLOTS; ++i) {
       mbar_init(&bar_q_full[i], 1);
@@ -82,7 +86,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
     }
     for (int i = 0; i < POBS_LSE_SLOTS; ++i) {
       mbar_init(&bar_l_full[i], 2);
-      mbar_init(&bar_l_free[i], 8);
+      mbar_init(&bar_l_free[i], 16);
     }
     fence_mbar_init();
   }
@@ -170,9 +174,13 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
         const uint32_t st = step % POBS_LSE_SLOTS;
         const int g = s / p.q_tiles, t = (s - g * p.q_tiles) * 128 + at;
         const float* src = p.lse + static_cast<size_t>(w.head * p.group + g) * p.n_queries + t;
-        float2 v;  // queries behind the last weigh nothing
-        v.x = t < p.n_queries ? -1.4426950408889634f * src[0] : -INFINITY;
-        v.y = t + 1 < p.n_queries ? -1.4426950408889634f * src[1] : -INFINITY;
+        // Queries behind the last weigh nothing, nor does one with a log-sum-exp of infinity: far below every logit, but finite
+        // (see the polynomial).  A NaN stays one.
+        float2 v;
+        v.x = t < p.n_queries ? -1.4426950408889634f * src[0] : WEIGHS_NOTHING;
+        v.y = t + 1 < p.n_queries ? -1.4426950408889634f * src[1] : WEIGHS_NOTHING;
+        v.x = v.x < WEIGHS_NOTHING ? WEIGHS_NOTHING : v.x > -WEIGHS_NOTHING ? -WEIGHS_NOTHING : v.x;
+        v.y = v.y < WEIGHS_NOTHING ? WEIGHS_NOTHING : v.y > -WEIGHS_NOTHING ? -WEIGHS_NOTHING : v.y;
         if (!(ok = mbar_wait_warp(&bar_l_free[st], ((step / POBS_LSE_SLOTS) & 1) ^ 1, abortp, p.c.status, 86))) break;
         *reinterpret_cast<float2*>(lse_ring + st * 128 + at) = v;
         __syncwarp();
@@ -225,27 +233,28 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
     }
   } else {
     // ------------------------------------------------------------------ sums: one thread per token
-    const int t = (warp - 8) >> 2, r = ((warp & 3) << 5) | lane;
-    const uint32_t s_addr = tmem + (static_cast<uint32_t>((warp & 3) << 5) << 16) + t * 128;
+    const int t = ((warp - 8) >> 2) & 1, r = ((warp & 3) << 5) | lane, half = (warp - 8) >> 3;
+    const uint32_t s_addr = tmem + (static_cast<uint32_t>((warp & 3) << 5) << 16) + t * 128 + half * 64;
     const uint64_t c2 = pack_f32x2(p.scale_log2e, p.scale_log2e);
     uint32_t step = 0;
     bool ok = true;
-    while (ok && x < x_hi) {
+    while (x < x_hi) {
       const ObserveItem w = observe_item(p, blockIdx.x, x, x_hi, head);
       const int token = w.pair * 256 + t * 128 + r;
       const bool tile_there = p.len.n[w.head] - w.pair * 256 > t * 128;
       float sum = 0.f;
       for (int s = w.begin; s < w.end; ++s, ++step) {
         const uint32_t st = step % POBS_LSE_SLOTS, buf = step & 1;
-        if (!(ok = mbar_wait_warp(&bar_l_full[st], (step / POBS_LSE_SLOTS) & 1, abortp, p.c.status, 88))) break;
-        if (!(ok = mbar_wait_warp(&bar_s_full[buf], (step >> 1) & 1, abortp, p.c.status, 89))) break;
+        if (ok) ok = mbar_wait_warp(&bar_l_full[st], (step / POBS_LSE_SLOTS) & 1, abortp, p.c.status, 88);
+        if (ok) ok = mbar_wait_warp(&bar_s_full[buf], (step >> 1) & 1, abortp, p.c.status, 89);
+        if (!ok) break;
         tc_fence_after_sync();
-        const int columns = min(128, p.n_queries - (s % p.q_tiles) * 128);
-        if (tile_there) {
-          const float4* l4 = reinterpret_cast<const float4*>(lse_ring + st * 128);
+        const int columns = min(128, p.n_queries - (s % p.q_tiles) * 128) - half * 64;
+        if (tile_there && columns > 0) {
+          const float4* l4 = reinterpret_cast<const float4*>(lse_ring + st * 128 + half * 64);
           uint64_t acc[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
 #pragma unroll 1
-          for (int ch = 0; ch * 32 < columns; ++ch) {
+          for (int ch = 0; ch * 32 < columns && ch < 2; ++ch) {
             uint32_t v[32];
             tmem_ld32(s_addr + buf * 256 + ch * 32, v);
             tmem_wait_ld(v);
@@ -258,16 +267,15 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
                                               k ? pack_f32x2(l.z, l.w) : pack_f32x2(l.x, l.y));
                 float x0, x1, e0, e1;
                 unpack_f32x2(x2, x0, x1);
-                if (k == 1 && (i & 1)) {
-                  ex2_poly5_pair(pack_f32x2(fmaxf(x0, -126.f), fmaxf(x1, -126.f)), e0, e1);
-                  // a NaN stays one, and what has no place below the largest float becomes infinity
-                  e0 = x0 <= 126.f ? e0 : x0 * INFINITY;
-                  e1 = x1 <= 126.f ? e1 : x1 * INFINITY;
+                if (k == 1 && (i & POBS_POLY_MASK) == POBS_POLY_MASK) {
+                  // held within the exponents of a float (2^128 is infinity); a NaN, which that would drop, comes back through the product with zero
+                  ex2_poly5_pair(pack_f32x2(fminf(fmaxf(x0, -126.f), 128.f), fminf(fmaxf(x1, -126.f), 128.f)), e0, e1);
+                  acc[k] = add_f32x2(acc[k], fma_f32x2(x2, pack_f32x2(0.f, 0.f), pack_f32x2(e0, e1)));
                 } else {
                   e0 = ex2_approx(x0);
                   e1 = ex2_approx(x1);
+                  acc[k] = add_f32x2(acc[k], pack_f32x2(e0, e1));
                 }
-                acc[k] = add_f32x2(acc[k], pack_f32x2(e0, e1));
               }
             }
           }
@@ -280,13 +288,19 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
         mbar_arrive_if(&bar_s_free[buf], lane == 0);
         mbar_arrive_if(&bar_l_free[st], lane == 0);
       }
-      if (!ok) break;
-      if (w.slot >= 0) {
-        p.part[static_cast<size_t>(w.slot) * 256 + t * 128 + r] = sum;
-      } else if (token < p.len.n[w.head]) {
-        float* dst = p.c.weights + static_cast<size_t>(w.head) * p.c.cap + token;
-        *dst = (p.decay == 0.f ? 0.f : p.decay * *dst) + sum;
+      // the two halves of a token's columns become one (these barriers are met whatever the waits gave)
+      if (half) other_half[t * 128 + r] = sum;
+      asm volatile("bar.sync 1, 512;" ::: "memory");
+      if (!half && ok) {
+        sum += other_half[t * 128 + r];
+        if (w.slot >= 0) {
+          p.part[static_cast<size_t>(w.slot) * 256 + t * 128 + r] = sum;
+        } else if (token < p.len.n[w.head]) {
+          float* dst = p.c.weights + static_cast<size_t>(w.head) * p.c.cap + token;
+          *dst = (p.decay == 0.f ? 0.f : p.decay * *dst) + sum;
+        }
       }
+      asm volatile("bar.sync 1, 512;" ::: "memory");
     }
   }
   tc_fence_before_sync();

@@ -266,6 +266,30 @@ def test_results_do_not_vary_between_calls_streams_and_replays():
         assert torch.equal(o, out) and torch.equal(l, lse) and torch.equal(cache.weights, weights)
 
 
+@pytest.mark.parametrize("heads,kv,n_q,n,d", [(12, 12, 300, 4000, 64), (16, 4, 77, 10007, 64), (12, 12, 300, 4000, 128), (12, 12, 512, 4000, 128), (12, 12, 1, 9000, 128),
+                                              (4, 1, 4, 9000, 64)])
+def test_the_same_call_again_and_again(heads, kv, n_q, n, d):
+    """Rings of shared memory whose slots are filled again while others are read: every one of many calls gives the same bits."""
+    import torch
+    g = gen(n)
+    k, v, q = randn(g, n, kv, d), randn(g, n, kv, d), randn(g, n_q, heads, d)
+    cache = make(heads, kv, d, n, k, v)
+    out, lse = attend(cache, q)
+    ref.check_attend(out, lse, q, per_head(k), per_head(v))
+    cache.observe(q, lse, decay=0.0)
+    weights = cache.weights.clone()
+    for wait in (False, True):
+        results = []
+        for _ in range(100):
+            o, l = torch.empty_like(out), torch.empty_like(lse)
+            cache.attend(q, o, l)
+            cache.observe(q, l, decay=0.0)
+            results.append((o, l, cache.weights.clone()))
+            if wait:
+                torch.cuda.synchronize()
+        assert all(torch.equal(o, out) and torch.equal(l, lse) and torch.equal(w, weights) for o, l, w in results)
+
+
 # ---------------------------------------------------------------------------------------------- accumulated weights
 
 
