@@ -140,11 +140,11 @@ int attend_few(headcast_packed* c, const void* q, void* out, float* lse, int32_t
   p.n_cta = std::min(c->n_sm, total);
   if (total > 0) {
     const bool one = p.n_rows <= 8;
-    const int smem = one ? RowsSmem<D, 1>::DYN_BYTES : RowsSmem<D, 2>::DYN_BYTES;
+    const int smem = RowsSmem<D>::DYN_BYTES;
     auto* kernel = one ? packed_rows_kernel<D, 1> : packed_rows_kernel<D, 2>;
     const int rc = allow_smem(c, one ? KERNEL_ROWS : KERNEL_ROWS_16, kernel, smem);
     if (rc != HC_OK) return rc;
-    PK_CUDA(c, launch_pdl(kernel, dim3(p.n_cta), dim3(rows_threads(one ? 1 : 2)), smem, st, p));
+    PK_CUDA(c, launch_pdl(kernel, dim3(p.n_cta), dim3(ROWS_THREADS), smem, st, p));
   }
   PK_CUDA(c, launch_pdl(packed_merge_rows_kernel<D>, dim3(p.n_rows, c->cfg.n_kv_heads), dim3(MERGE_GROUPS * D / 4), 0, st, p));
   return HC_OK;

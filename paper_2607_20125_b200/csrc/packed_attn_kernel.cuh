@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
   constexpr int QK_STEPS = D / 16;
   constexpr uint32_t TMEM_COLS = 512;
   constexpr uint32_t S_COL = 0, O_COL = 256;  // S_t at t*128, O_t at 256 + t*128; P_t overlays the first half of S_t
-  constexpr int P_HEAD = 2;                   // of the four 32-token chunks of P, how many are handed over ahead of the rest
+  constexpr int P_HEAD = 1;                   // of the four 32-token chunks of P, how many are handed over ahead of the rest (30 x 52 block: 1: 805 us, 2: 833, 3: 820)
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));

@@ -253,8 +253,9 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
         if (tile_there && columns > 0) {
           const float4* l4 = reinterpret_cast<const float4*>(lse_ring + st * 128 + half * 64);
           uint64_t acc[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
-#pragma unroll 1
-          for (int ch = 0; ch * 32 < columns && ch < 2; ++ch) {
+#pragma unroll
+          for (int ch = 0; ch < 2; ++ch) {
+            if (ch * 32 >= columns) break;
             uint32_t v[32];
             tmem_ld32(s_addr + buf * 256 + ch * 32, v);
             tmem_wait_ld(v);

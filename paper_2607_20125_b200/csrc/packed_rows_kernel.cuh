@@ -20,9 +20,8 @@ namespace hc {
 
 constexpr int ROWS_MAX = 16;
 constexpr int ROWS_GROUP_WARPS = 8;
-// Groups of warps: with one tile of queries three fit (80 registers a thread), with two tiles two (128).
-__host__ __device__ constexpr int rows_groups(int nq) { return nq == 1 ? 3 : 2; }
-__host__ __device__ constexpr int rows_threads(int nq) { return rows_groups(nq) * ROWS_GROUP_WARPS * 32; }
+constexpr int ROWS_GROUPS = 2;  // of warps (a third one, at 80 registers a thread, made the call for one token 9 % slower)
+constexpr int ROWS_THREADS = ROWS_GROUPS * ROWS_GROUP_WARPS * 32;
 struct PackedRowsParams {
   PackedView c;
   const __nv_bfloat16* q;  // [n_queries][n_kv * group][d]; row r of head h is token r / group, head h * group + r % group
@@ -43,14 +42,14 @@ __device__ __forceinline__ uint32_t turn_8x8(uint32_t v) {
   return d;
 }
 
-template <int D, int NQ>
+template <int D>
 struct RowsSmem {
   static constexpr int CODES = PACK_TILE * D / 2, SCALES = PACK_TILE * D / PACK_GROUP;
   static constexpr int STAGE = 2 * (CODES + SCALES);  // K codes, V codes, K scales, V scales
   static constexpr int STAGES = D == 128 ? 6 : 12;    // a multiple of the groups: a stage belongs to one of them
   static constexpr int Q_OFF = STAGES * STAGE;        // [D / 16][2 query tiles][32 lanes] uint2
   static constexpr int MERGE_OFF = Q_OFF + D / 16 * 512;
-  static constexpr int MERGE = rows_groups(NQ) * ROWS_GROUP_WARPS * 8 * D * 4;
+  static constexpr int MERGE = ROWS_GROUPS * ROWS_GROUP_WARPS * 8 * D * 4;
   static constexpr int DYN_BYTES = MERGE_OFF + MERGE + 128;
 };
 
@@ -92,9 +91,9 @@ __device__ __forceinline__ void stage_row(uint2* qs, float* row_scale, const __n
 
 // NQ: tiles of eight query rows
 template <int D, int NQ>
-__global__ void __launch_bounds__(rows_threads(NQ), 1) packed_rows_kernel(const __grid_constant__ PackedRowsParams p) {
-  using SM = RowsSmem<D, NQ>;
-  constexpr int GROUPS = rows_groups(NQ), WARPS = GROUPS * ROWS_GROUP_WARPS;
+__global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __grid_constant__ PackedRowsParams p) {
+  using SM = RowsSmem<D>;
+  constexpr int GROUPS = ROWS_GROUPS, WARPS = GROUPS * ROWS_GROUP_WARPS;
   constexpr int KW = D / 32;  // words of a key row that a lane reads
   constexpr int W = D / 8;    // elements of a value row that a lane reads
   constexpr int NT = D / 16;  // row tiles of O^T
@@ -229,11 +228,15 @@ __global__ void __launch_bounds__(rows_threads(NQ), 1) packed_rows_kernel(const 
           if (8 + key_row >= last_valid) s[z][2] = s[z][3] = -INFINITY;
         }
       }
-      // The reference moves only when some logit outgrows it (c may be NaN, never negative); tokens that are not there leave it.
+      // The reference moves only when some logit outgrows it (a NaN never does); tokens that are not there leave it.
+      float x[NQ][4];
       bool grow = false;
 #pragma unroll
-      for (int z = 0; z < NQ; ++z)
-        grow |= fmaxf(s[z][0], s[z][2]) * c[z][0] > m[z][0] + P_LAG || fmaxf(s[z][1], s[z][3]) * c[z][1] > m[z][1] + P_LAG;
+      for (int z = 0; z < NQ; ++z) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x[z][y] = fmaf(s[z][y], c[z][y & 1], -m[z][y & 1]);
+        grow |= fmaxf(fmaxf(x[z][0], x[z][1]), fmaxf(x[z][2], x[z][3])) > P_LAG;
+      }
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int z = 0; z < NQ; ++z)
@@ -253,12 +256,15 @@ __global__ void __launch_bounds__(rows_threads(NQ), 1) packed_rows_kernel(const 
               o[z][x][y + 2] *= f;
             }
           }
+#pragma unroll
+        for (int z = 0; z < NQ; ++z)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) x[z][y] = fmaf(s[z][y], c[z][y & 1], -m[z][y & 1]);
       }
       uint32_t pt[NQ][2];  // P^T as the products want it: two tokens of one query
 #pragma unroll
       for (int z = 0; z < NQ; ++z) {
-        const float e0 = ex2_approx(fmaf(s[z][0], c[z][0], -m[z][0])), e1 = ex2_approx(fmaf(s[z][1], c[z][1], -m[z][1]));
-        const float e2 = ex2_approx(fmaf(s[z][2], c[z][0], -m[z][0])), e3 = ex2_approx(fmaf(s[z][3], c[z][1], -m[z][1]));
+        const float e0 = ex2_approx(x[z][0]), e1 = ex2_approx(x[z][1]), e2 = ex2_approx(x[z][2]), e3 = ex2_approx(x[z][3]);
         l[z][0] += e0 + e2;
         l[z][1] += e1 + e3;
         pt[z][0] = turn_8x8(pack_f16x2(e0, e1));
