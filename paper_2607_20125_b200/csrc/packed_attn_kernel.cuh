@@ -5,7 +5,7 @@
 // warp - with the tile loads replaced by four warps that turn codes into operands:
 //   - codes and scales arrive in shared memory by bulk copies, up to three tiles ahead; the warps convert them to fp16 (exact) and
 //     write them into a ring slot in the layout that the products read (128-byte swizzle).  (Fetched into registers instead, a tile
-//     took 1600 clk to convert: the fence behind its stores also waits for the loads that are under way for the next.);
+//     took 1600 clk to convert: the fence behind its stores also waits for the loads that are under way for the next.)
 //   - all operands are fp16: rows of Q are brought to a common power of two first (exact but for elements below 2^-28 of
 //     their row's largest), P keeps 11 bits, so the row sum needs no rounding of its own to match;
 //   - 56 / 72 / 192 / 192 registers for the issuing, converting and the two softmax warpgroups.
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
   constexpr int P_HEAD = 1;                   // of the four 32-token chunks of P, how many are handed over ahead of the rest (30 x 52 block: 1: 805 us, 2: 833, 3: 820)
 
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* smem = aligned_shared<1024>(smem_raw);
   __shared__ uint64_t bar_q_full[2], bar_s_full[2], bar_p_head[2], bar_p_full[2], bar_o_full[2];
   __shared__ uint64_t bar_kv_full[PATTN_SLOTS], bar_kv_free[PATTN_SLOTS], bar_c_full[PATTN_CODE_SLOTS], bar_c_free[PATTN_CODE_SLOTS];
   __shared__ uint32_t tmem_slot;
@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
     constexpr int PARTS = D / 32, ROWS = 32 / PARTS, PASSES = 32 / ROWS;
     const int part = lane % PARTS;
     const bool swap = PARTS == 4 && part >= 2;
+    const int row0 = (warp & 3) * 32 + lane / PARTS;
     uint32_t g = 0;
     bool ok = true;
     while (ok && x < x_hi) {
@@ -248,21 +249,24 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         const uint32_t cs = g % PATTN_CODE_SLOTS, st = g % PATTN_SLOTS;
         if (!(ok = mbar_wait_warp(&bar_c_full[cs], (g / PATTN_CODE_SLOTS) & 1, abortp, p.c.status, 77))) break;
         const uint8_t* codes = smem + SM::CODE_OFF + cs * SM::CODE_BYTES;
-        uint4 c[PASSES];
-        uint32_t sc[PASSES];
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-          const int row = (warp & 3) * 32 + i * ROWS + lane / PARTS;
-          c[i] = *reinterpret_cast<const uint4*>(codes + row * (D / 2) + part * 16);
-          sc[i] = *reinterpret_cast<const uint16_t*>(codes + PACK_TILE * D / 2 + row * (D / PACK_GROUP) + part * 2);
-        }
         if (!(ok = mbar_wait_warp(&bar_kv_free[st], ((g / PATTN_SLOTS) & 1) ^ 1, abortp, p.c.status, 80))) break;
         uint8_t* dst = smem + SM::KV_OFF + st * SM::TILE_BYTES + (part / 2) * SM::BLOCK_BYTES;
-#pragma unroll
+        // one pass at a time, its words fetched during the one before: unrolled, the code of all roles together ran 7 % slower
+        const uint8_t* at = codes + row0 * (D / 2) + part * 16;
+        const uint8_t* at_scales = codes + PACK_TILE * D / 2 + row0 * (D / PACK_GROUP) + part * 2;
+        uint4 c_next = *reinterpret_cast<const uint4*>(at);
+        uint32_t sc_next = *reinterpret_cast<const uint16_t*>(at_scales);
+#pragma unroll 1
         for (int i = 0; i < PASSES; ++i) {
-          const int row = (warp & 3) * 32 + i * ROWS + lane / PARTS;
-          const uint32_t words[4] = {swap ? c[i].z : c[i].x, swap ? c[i].w : c[i].y, swap ? c[i].x : c[i].z, swap ? c[i].y : c[i].w};
-          const uint32_t s_lo = scale_f16x2(sc[i], 0), s_hi = scale_f16x2(sc[i], 1);
+          const uint4 c = c_next;
+          const uint32_t sc = sc_next;
+          if (i + 1 < PASSES) {
+            c_next = *reinterpret_cast<const uint4*>(at + (i + 1) * ROWS * (D / 2));
+            sc_next = *reinterpret_cast<const uint16_t*>(at_scales + (i + 1) * ROWS * (D / PACK_GROUP));
+          }
+          const int row = row0 + i * ROWS;
+          const uint32_t words[4] = {swap ? c.z : c.x, swap ? c.w : c.y, swap ? c.x : c.z, swap ? c.y : c.w};
+          const uint32_t s_lo = scale_f16x2(sc, 0), s_hi = scale_f16x2(sc, 1);
           const uint32_t s2[2] = {swap ? s_hi : s_lo, swap ? s_lo : s_hi};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -303,38 +307,29 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         const int token = (base + r) / p.group;
         at = static_cast<int64_t>(token) * heads + w.head * p.group + (base + r - token * p.group);
       }
-      // ---- this warp's 32 query rows, as fp16 relative to a power of two of their own, into shared memory (swizzled); invalid rows are
-      // zero.  CH consecutive lanes share a row.
-      float c = 0.f;  // from logits to the log2 domain
+      // ---- this thread's query row, as fp16 relative to a power of two of its own, into shared memory (swizzled); invalid rows are zero
+      float c;  // from logits to the log2 domain
       {
         constexpr int CH = D / 8;
         uint4 v[CH];
 #pragma unroll
-        for (int k = 0; k < CH; ++k) {
-          const int idx = k * 32 + lane, row = idx / CH, ch = idx % CH;
-          const int64_t from = __shfl_sync(0xffffffffu, at, row);
-          const bool valid = __shfl_sync(0xffffffffu, row_valid ? 1 : 0, row) != 0;
-          v[k] = make_uint4(0, 0, 0, 0);
-          if (valid) v[k] = *(reinterpret_cast<const uint4*>(p.q + from * D) + ch);
-        }
+        for (int k = 0; k < CH; ++k) v[k] = row_valid ? *(reinterpret_cast<const uint4*>(p.q + at * D) + k) : make_uint4(0, 0, 0, 0);
+        // the largest magnitude as an integer: bf16 magnitudes are ordered like their bits, NaN above infinity
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+          top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[k].x & 0x7fff7fffu, v[k].y & 0x7fff7fffu)), __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu));
+        top = max(top & 0xffffu, top >> 16);
+        float f, back;
+        row_factor(__uint_as_float(top << 16), f, back);
+        c = p.scale_log2e * back;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-          const int idx = k * 32 + lane, row = idx / CH, ch = idx % CH;
           const uint32_t raw[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-          // the largest magnitude as an integer: bf16 magnitudes are ordered like their bits, NaN above infinity
-          uint32_t top = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top = max(top, max(raw[i] & 0x7fffu, (raw[i] >> 16) & 0x7fffu));
-#pragma unroll
-          for (int o = 1; o < CH; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          float f, back;
-          row_factor(__uint_as_float(top << 16), f, back);
-          const float theirs = __shfl_sync(0xffffffffu, back, (lane % (32 / CH)) * CH);
-          if (lane / (32 / CH) == k) c = p.scale_log2e * theirs;
           uint32_t y[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) y[i] = pack_f16x2(__uint_as_float(raw[i] << 16) * f, __uint_as_float(raw[i] & 0xffff0000u) * f);
-          *reinterpret_cast<uint4*>(sq + (ch / 8) * SM::BLOCK_BYTES + sw128_offset(row0 + row, ch % 8)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(sq + (k / 8) * SM::BLOCK_BYTES + sw128_offset(r, k % 8)) = make_uint4(y[0], y[1], y[2], y[3]);
         }
         fence_proxy_async_smem();
         tc_fence_before_sync();  // orders this thread's TMEM reads of the previous item before the arrive
@@ -355,6 +350,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
           for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_addr + ch * 32, sv[ch]);
           tmem_wait_ld(sv[0], sv[1], sv[2], sv[3]);
           if (n_valid < PACK_TILE) {  // the last tile of a head: one branch for the whole tile
+            asm volatile("" ::: "memory");  // (a branch it stays: as selections it cost every tile 128 of them)
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
@@ -453,7 +449,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         }
         __syncwarp();
         constexpr int U = D / 8;
-#pragma unroll
+#pragma unroll 4
         for (int k = 0; k < U; ++k) {
           const int idx = k * 32 + lane, row = idx / U, u = idx % U;
           const uint4 val = *reinterpret_cast<const uint4*>(stg + (u / 8) * SM::BLOCK_BYTES + row * 128 + (((u % 8) ^ (row & 7)) << 4));

@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
   using SM = ObserveSmem<D>;
   constexpr uint32_t TMEM_COLS = 512;  // two buffers of two 128-column products
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* smem = aligned_shared<1024>(smem_raw);
   __shared__ uint64_t bar_k_full[2], bar_k_free[2], bar_q_full[SM::Q_SLOTS], bar_q_free[SM::Q_SLOTS], bar_l_full[POBS_LSE_SLOTS], bar_l_free[POBS_LSE_SLOTS],
       bar_s_full[2], bar_s_free[2];
   __shared__ uint32_t tmem_slot;
@@ -124,12 +124,12 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
       const ObserveItem w = observe_item(p, blockIdx.x, x, x_hi, head);
       const bool two = p.len.n[w.head] - w.pair * 256 > 128;
       const uint32_t kb = item & 1;
-      if (!(ok = wait(&bar_k_full[kb], (item >> 1) & 1, 81))) break;
+      if (!(ok = wait(&bar_k_full[kb], (item >> 1) & 1, 101))) break;
       ++item;
       for (int s = w.begin; s < w.end; ++s, ++step) {
         const uint32_t st = step % SM::Q_SLOTS, buf = step & 1;
-        if (!(ok = wait(&bar_q_full[st], (step / SM::Q_SLOTS) & 1, 82))) break;
-        if (!(ok = wait(&bar_s_free[buf], ((step >> 1) & 1) ^ 1, 83))) break;
+        if (!(ok = wait(&bar_q_full[st], (step / SM::Q_SLOTS) & 1, 102))) break;
+        if (!(ok = wait(&bar_s_free[buf], ((step >> 1) & 1) ^ 1, 103))) break;
         tc_fence_after_sync();
         const uint64_t q_at = q_desc + ((st * SM::TILE_BYTES) >> 4), k_at = k_desc + ((2 * kb * SM::TILE_BYTES) >> 4);
         mma_block_ss<D / 16>(tmem + buf * 256, k_at, q_at, idesc, SM::BLOCK_BYTES >> 4, elected);
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
         const ObserveItem w = observe_item(p, blockIdx.x, x, x_hi, head);
         for (int s = w.begin; s < w.end; ++s, ++step) {
           const uint32_t st = step % SM::Q_SLOTS;
-          if (!(ok = mbar_wait(&bar_q_free[st], ((step / SM::Q_SLOTS) & 1) ^ 1, abortp, p.c.status, 84))) break;
+          if (!(ok = mbar_wait(&bar_q_free[st], ((step / SM::Q_SLOTS) & 1) ^ 1, abortp, p.c.status, 104))) break;
           mbar_arrive_expect_tx(&bar_q_full[st], SM::TILE_BYTES);
           const int g = s / p.q_tiles, row = (s - g * p.q_tiles) * 128;
           for (int b = 0; b < D / 64; ++b)
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
       if (!ok) {
         for (uint32_t back = 1; back <= SM::Q_SLOTS && back <= step; ++back) {  // the copies in flight land before the block leaves
           int local_abort = 0;
-          mbar_wait(&bar_q_full[(step - back) % SM::Q_SLOTS], ((step - back) / SM::Q_SLOTS) & 1, &local_abort, p.c.status, 85);
+          mbar_wait(&bar_q_full[(step - back) % SM::Q_SLOTS], ((step - back) / SM::Q_SLOTS) & 1, &local_abort, p.c.status, 105);
         }
       }
     }
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
         v.y = t + 1 < p.n_queries ? -1.4426950408889634f * src[1] : WEIGHS_NOTHING;
         v.x = v.x < WEIGHS_NOTHING ? WEIGHS_NOTHING : v.x > -WEIGHS_NOTHING ? -WEIGHS_NOTHING : v.x;
         v.y = v.y < WEIGHS_NOTHING ? WEIGHS_NOTHING : v.y > -WEIGHS_NOTHING ? -WEIGHS_NOTHING : v.y;
-        if (!(ok = mbar_wait_warp(&bar_l_free[st], ((step / POBS_LSE_SLOTS) & 1) ^ 1, abortp, p.c.status, 86))) break;
+        if (!(ok = mbar_wait_warp(&bar_l_free[st], ((step / POBS_LSE_SLOTS) & 1) ^ 1, abortp, p.c.status, 106))) break;
         *reinterpret_cast<float2*>(lse_ring + st * 128 + at) = v;
         __syncwarp();
         mbar_arrive_if(&bar_l_full[st], lane == 0);
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) scales[t][i] = sc[i];
       }
-      if (!(ok = mbar_wait_warp(&bar_k_free[kb], ((item >> 1) & 1) ^ 1, abortp, p.c.status, 87))) break;
+      if (!(ok = mbar_wait_warp(&bar_k_free[kb], ((item >> 1) & 1) ^ 1, abortp, p.c.status, 107))) break;
       ++item;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -245,8 +245,8 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
       float sum = 0.f;
       for (int s = w.begin; s < w.end; ++s, ++step) {
         const uint32_t st = step % POBS_LSE_SLOTS, buf = step & 1;
-        if (ok) ok = mbar_wait_warp(&bar_l_full[st], (step / POBS_LSE_SLOTS) & 1, abortp, p.c.status, 88);
-        if (ok) ok = mbar_wait_warp(&bar_s_full[buf], (step >> 1) & 1, abortp, p.c.status, 89);
+        if (ok) ok = mbar_wait_warp(&bar_l_full[st], (step / POBS_LSE_SLOTS) & 1, abortp, p.c.status, 108);
+        if (ok) ok = mbar_wait_warp(&bar_s_full[buf], (step >> 1) & 1, abortp, p.c.status, 109);
         if (!ok) break;
         tc_fence_after_sync();
         const int columns = min(128, p.n_queries - (s % p.q_tiles) * 128) - half * 64;

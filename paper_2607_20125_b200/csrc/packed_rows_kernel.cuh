@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
   constexpr int W = D / 8;    // elements of a value row that a lane reads
   constexpr int NT = D / 16;  // row tiles of O^T
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));
+  uint8_t* smem = aligned_shared<128>(smem_raw);
   __shared__ uint64_t bar_full[SM::STAGES];
   __shared__ int done[SM::STAGES], loads[SM::STAGES];  // warps that have left a stage's tile; copies into the stage so far
   __shared__ int abort_flag;
