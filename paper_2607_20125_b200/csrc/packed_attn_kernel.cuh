@@ -58,6 +58,7 @@ constexpr int PATTN_REGS_LAUNCH = 128, PATTN_REGS_ISSUE = 56, PATTN_REGS_CONVERT
 static_assert(PATTN_REGS_ISSUE + PATTN_REGS_CONVERT + 2 * PATTN_REGS_SOFTMAX <= 4 * PATTN_REGS_LAUNCH, "the block cannot take more registers than it was launched with");
 constexpr int PATTN_SLOTS = 4;       // ring of converted K and V tiles, K0 V0 K1 V1 ...
 constexpr int PATTN_CODE_SLOTS = 3;  // and of their codes on the way in
+constexpr float P_MOST = 32768.f;    // of a tile's sum of exponentials without a new reference: each then fits fp16, whose largest is 65504
 
 // 2^f on [-1/2, 1/2]: of the polynomials with value 1 at 0 (whole powers come out exact, 2^128 as infinity) the one of least largest
 // relative error (Lawson's iteration on 4001 Chebyshev points), coefficients rounded to fp32
@@ -97,11 +98,10 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
   constexpr int QK_STEPS = D / 16;
   constexpr uint32_t TMEM_COLS = 512;
   constexpr uint32_t S_COL = 0, O_COL = 256;  // S_t at t*128, O_t at 256 + t*128; P_t overlays the first half of S_t
-  constexpr int P_HEAD = 1;                   // of the four 32-token chunks of P, how many are handed over ahead of the rest (30 x 52 block: 1: 805 us, 2: 833, 3: 820)
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = aligned_shared<1024>(smem_raw);
-  __shared__ uint64_t bar_q_full[2], bar_s_full[2], bar_p_head[2], bar_p_full[2], bar_o_full[2];
+  __shared__ uint64_t bar_q_full[2], bar_s_full[2], bar_p_full[2], bar_o_full[2];
   __shared__ uint64_t bar_kv_full[PATTN_SLOTS], bar_kv_free[PATTN_SLOTS], bar_c_full[PATTN_CODE_SLOTS], bar_c_free[PATTN_CODE_SLOTS];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
@@ -111,7 +111,6 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
     for (int t = 0; t < 2; ++t) {
       mbar_init(&bar_q_full[t], 4);
       mbar_init(&bar_s_full[t], 1);
-      mbar_init(&bar_p_head[t], 4);
       mbar_init(&bar_p_full[t], 4);
       mbar_init(&bar_o_full[t], 1);
     }
@@ -186,13 +185,10 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
           if (j + 1 < nt && !(ok = wait(&bar_kv_full[st1], ph1, 74))) break;
           for (int t = 0; t < n_q && ok; ++t) {
             const uint64_t v_at = v_desc + ((st * SM::TILE_BYTES) >> 4);
-            if (!(ok = wait(&bar_p_head[t], p_cnt[t] & 1, 75))) break;
-            tc_fence_after_sync();
-            mma_block_ts<0, 2 * P_HEAD>(tmem + O_COL + t * 128, tmem + S_COL + t * 128, v_at, idesc_o, j > 0 ? 1u : 0u, elected);
             if (!(ok = wait(&bar_p_full[t], p_cnt[t] & 1, 76))) break;
             ++p_cnt[t];
             tc_fence_after_sync();
-            mma_block_ts<2 * P_HEAD, 8>(tmem + O_COL + t * 128, tmem + S_COL + t * 128, v_at, idesc_o, 1u, elected);
+            mma_block_ts<0, 8>(tmem + O_COL + t * 128, tmem + S_COL + t * 128, v_at, idesc_o, j > 0 ? 1u : 0u, elected);
             if (j + 1 < nt) {
               issue_qk(t, st1);
               mma_commit(&bar_s_full[t], elected);
@@ -336,93 +332,92 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         __syncwarp();
         mbar_arrive_if(&bar_q_full[t], lane == 0);
       }
-      float m_ref = -INFINITY, l_sum = 0.f;
+      float m_ref = NO_REFERENCE, l_sum = 0.f;
       for (int tile = w.tile_begin; tile < w.tile_end; ++tile) {
         const int n_valid = min(PACK_TILE, p.len.n[w.head] - tile * PACK_TILE);
         if (!(ok = mbar_wait_warp(&bar_s_full[t], s_cnt & 1, abortp, p.c.status, 78))) break;
         ++s_cnt;
         tc_fence_after_sync();
-        uint32_t sv[4][32];
-        float mx;
-        {
-          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_addr + ch * 32, sv[ch]);
-          tmem_wait_ld(sv[0], sv[1], sv[2], sv[3]);
-          if (n_valid < PACK_TILE) {  // the last tile of a head: one branch for the whole tile
-            asm volatile("" ::: "memory");  // (a branch it stays: as selections it cost every tile 128 of them)
-#pragma unroll
-            for (int ch = 0; ch < 4; ++ch)
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (ch * 32 + i >= n_valid) sv[ch][i] = 0xff800000u;
-          }
-#pragma unroll
-          for (int ch = 0; ch < 4; ++ch)
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              mx4[0] = max3(mx4[0], __uint_as_float(sv[ch][i]), __uint_as_float(sv[ch][i + 1]));
-              mx4[1] = max3(mx4[1], __uint_as_float(sv[ch][i + 2]), __uint_as_float(sv[ch][i + 3]));
-              mx4[2] = max3(mx4[2], __uint_as_float(sv[ch][i + 4]), __uint_as_float(sv[ch][i + 5]));
-              mx4[3] = max3(mx4[3], __uint_as_float(sv[ch][i + 6]), __uint_as_float(sv[ch][i + 7]));
-            }
-          mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * c;
-        }
-        // the reference moves only when some row's maximum outgrows it
-        if (__any_sync(0xffffffffu, mx > m_ref + P_LAG)) {
-          const float m_new = mx > m_ref + P_HEADROOM ? mx - P_HEADROOM : m_ref;
-          const float alpha = (m_new == -INFINITY) ? 1.f : ex2_approx(m_ref - m_new);
-          l_sum *= alpha;
-          m_ref = m_new;
-          if (tile > w.tile_begin) {
+        if (n_valid < PACK_TILE) {  // the last tile of a head: the columns behind its tokens, in tensor memory and in a few instructions
 #pragma unroll 1
-            for (int ch = 0; ch < D / 16; ++ch) {
-              uint32_t v[16];
-              tmem_ld16(o_addr + ch * 16, v);
+          for (int i = n_valid; i < PACK_TILE; ++i) tmem_st1(s_addr + i, 0xff800000u);
+          tmem_wait_st();
+        }
+        // The exponentials are taken relative to the reference as it stands, without a look for the tile's maximum: their sum shows
+        // whether one of them outgrew fp16 (each is at most the sum).  Only then, and in an item's first tile, the maximum is
+        // found, the reference moved and the tile done again; the logits are still there, P is stored last.
+        uint32_t pk[64];
+        float tile_sum;
+        for (bool look = tile == w.tile_begin;; look = true) {
+          if (look) {
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int ch = 0; ch < 4; ++ch) {
+              uint32_t v[32];
+              tmem_ld32(s_addr + ch * 32, v);
               tmem_wait_ld(v);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-              tmem_st16(o_addr + ch * 16, v);
+              for (int i = 0; i < 32; i += 2) mx = max3(mx, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+            }
+            mx *= c;
+            if (__any_sync(0xffffffffu, mx > m_ref + P_HEADROOM + 1.f)) {
+              const float m_new = mx > m_ref + P_HEADROOM ? mx - P_HEADROOM : m_ref;
+              const float alpha = ex2_approx(m_ref - m_new);
+              l_sum *= alpha;
+              m_ref = m_new;
+              if (tile > w.tile_begin) {
+#pragma unroll 1
+                for (int ch = 0; ch < D / 16; ++ch) {
+                  uint32_t v[16];
+                  tmem_ld16(o_addr + ch * 16, v);
+                  tmem_wait_ld(v);
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                  tmem_st16(o_addr + ch * 16, v);
+                }
+              }
             }
           }
-        }
-        const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
-        const uint64_t c2 = pack_f32x2(c, c), m2 = pack_f32x2(-m_use, -m_use);
-        uint64_t sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
+          const uint64_t c2 = pack_f32x2(c, c), m2 = pack_f32x2(-m_ref, -m_ref);
+          uint64_t sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
+          uint32_t v[2][32];
+          tmem_ld32(s_addr, v[0]);
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
-          uint32_t pk[16];
+          for (int ch = 0; ch < 4; ++ch) {
+            tmem_wait_ld(v[ch & 1]);
+            if (ch < 3) tmem_ld32(s_addr + (ch + 1) * 32, v[(ch + 1) & 1]);  // on its way while these are worked on
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(sv[ch][2 * i]), __uint_as_float(sv[ch][2 * i + 1])), c2, m2);
-            float x0, x1, e0, e1;
-            unpack_f32x2(x2, x0, x1);
-            if ((i & 7) == 7) {
-              ex2_poly5_pair(pack_f32x2(fmaxf(x0, -126.f), fmaxf(x1, -126.f)), e0, e1);
-            } else {
-              e0 = ex2_approx(x0);
-              e1 = ex2_approx(x1);
+            for (int i = 0; i < 16; ++i) {
+              const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(v[ch & 1][2 * i]), __uint_as_float(v[ch & 1][2 * i + 1])), c2, m2);
+              float x0, x1, e0, e1;
+              unpack_f32x2(x2, x0, x1);
+              if ((i & 7) == 7) {
+                // (held within the exponents of a float; what is too large stays far too large)
+                ex2_poly5_pair(pack_f32x2(fminf(fmaxf(x0, -126.f), 126.f), fminf(fmaxf(x1, -126.f), 126.f)), e0, e1);
+              } else {
+                e0 = ex2_approx(x0);
+                e1 = ex2_approx(x1);
+              }
+              pk[16 * ch + i] = pack_f16x2(e0, e1);
+              sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(e0, e1));
             }
-            pk[i] = pack_f16x2(e0, e1);
-            sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(e0, e1));
           }
-          if (ch == P_HEAD) {
-            tmem_wait_st();
-            tc_fence_before_sync();
-            __syncwarp();
-            mbar_arrive_if(&bar_p_head[t], lane == 0);
-          }
-          tmem_st16(s_addr + ch * 16, pk);
+          float a0, a1;
+          unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a0, a1);
+          tile_sum = a0 + a1;
+          // (a row of NaNs looks every time, once)
+          if (look || !__any_sync(0xffffffffu, !(tile_sum <= P_MOST))) break;
         }
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) tmem_st16(s_addr + ch * 16, *reinterpret_cast<uint32_t(*)[16]>(&pk[16 * ch]));
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
         mbar_arrive_if(&bar_p_full[t], lane == 0);
-        float a0, a1;
-        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a0, a1);
-        l_sum += a0 + a1;
+        l_sum += tile_sum;
       }
       if (!ok) break;
+      if (m_ref == NO_REFERENCE) m_ref = -INFINITY;  // nothing but NaNs
       // ---- epilogue
       if (!(ok = mbar_wait_warp(&bar_o_full[t], o_cnt & 1, abortp, p.c.status, 79))) break;
       ++o_cnt;

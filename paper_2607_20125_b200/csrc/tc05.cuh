@@ -296,6 +296,9 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, uint32_t v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(v) : "memory");
+}
 // Waits for this thread's tensor-memory loads; the registers of the waited-for loads are operands, so that no use of them
 // can be scheduled ahead of the wait.
 __device__ __forceinline__ void tmem_wait_ld(uint32_t (&a)[16]) {
