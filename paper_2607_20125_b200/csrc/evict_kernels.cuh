@@ -2,10 +2,11 @@
 //
 // evict_select_kernel, one cluster of up to 8 blocks per head: the keep-th largest weight by radix selection (three digits of
 // 11, 11 and 10 bits of an order-preserving integer), then the places of all tokens above it, and of the first ones equal to it, in
-// order.  The blocks of a cluster split the head's tokens, add up their histograms through each other's shared memory, and each finds
-// the digit for itself.  Counts are integers and places follow from prefix sums, so the result is the same every time.
-// What it costs is latency: 4 bytes per token are read once from memory (again from L2 where a block's share exceeds
-// SELECT_KEYS), and a handful of cluster barriers follow one another.
+// order.  The blocks of a cluster split the head's tokens, a warp a run of them; each block finds the digit for itself from the
+// histograms of all, first among 64 sums of 32 bins, then among that group's bins, so that little crosses between the blocks (all
+// 2048 bins read from all blocks took 2.7 us a digit).  Counts are integers and places follow from prefix sums, so the result is
+// the same every time.  What it costs is latency: the weights are read once, into registers (again from L2 where a thread's share
+// exceeds SELECT_HELD), and a handful of cluster barriers follow one another.
 // evict_move_kernel copies the rows: bound by memory, 148 bytes read and written per token at d = 128.
 #pragma once
 #include "packed_format.cuh"
@@ -13,9 +14,8 @@
 namespace hc {
 
 constexpr int SELECT_THREADS = 1024;
-constexpr int SELECT_KEYS = 24576;  // keys that a block keeps in shared memory
-constexpr int SELECT_BINS = 2048;
-constexpr int SELECT_SMEM = SELECT_KEYS * 4 + 2 * SELECT_BINS * 4;
+constexpr int SELECT_HELD = 12;   // keys that a thread keeps in registers
+constexpr int SELECT_BINS = 2048, SELECT_GROUPS = 64;
 
 struct SelectParams {
   const float* weights;  // [n_kv][cap]
@@ -43,24 +43,50 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return r;
 }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-// Two words of another block's shared memory, at the place where `p` is in this one's.
-__device__ __forceinline__ uint2 peer_words(const uint32_t* p, uint32_t rank) {
-  uint32_t at;
-  uint2 v;
+// A word of another block's shared memory, at the place where `p` is in this one's.
+__device__ __forceinline__ uint32_t peer_word(const uint32_t* p, uint32_t rank) {
+  uint32_t at, v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
 }
 constexpr int SELECT_MAX_BLOCKS = 8;  // of a cluster
 
+// Of n counts (64 or 32, one per thread of the first warps), highest first: which one holds the k-th key, and the rank in it.  The whole
+// block calls it; the counts lie in `sums`, the answer goes to `found`.
+template <int N>
+__device__ __forceinline__ void find_kth(const uint32_t* sums, uint32_t k, uint32_t* found) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid < 32) {
+    constexpr int PER = N / 32;
+    uint32_t c[PER], total = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) total += c[i] = sums[tid * PER + i];
+    uint32_t suffix = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_down_sync(0xffffffffu, suffix, o);
+      if (tid + o < 32) suffix += up;
+    }
+    uint32_t above = suffix - total;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) {
+      if (above < k && k <= above + c[i]) {  // exactly one lane, once
+        found[0] = tid * PER + i;
+        found[1] = k - above;
+      }
+      above += c[i];
+    }
+  }
+  __syncthreads();
+}
+
 __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __grid_constant__ SelectParams p) {
-  extern __shared__ uint32_t select_smem[];
-  uint32_t* const keys = select_smem;
-  uint32_t* const hist = select_smem + SELECT_KEYS;  // two histograms, used in turn: one cluster barrier per digit
-  __shared__ uint32_t warp_sum[32], found[2], warp_gt[32], warp_eq[32];
-  __shared__ alignas(8) uint32_t counts[2];
+  __shared__ uint32_t hist[2][SELECT_BINS], groups[2][SELECT_GROUPS];  // used in turn: one cluster barrier per digit
+  __shared__ uint32_t sums[SELECT_GROUPS], found[2], counts[2], warp_gt[32], warp_eq[32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank(), ranks = cluster_size();
   const int h = blockIdx.x / ranks;
@@ -71,68 +97,93 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
   const int lo = static_cast<int>(static_cast<long long>(n) * rank / ranks), hi = static_cast<int>(static_cast<long long>(n) * (rank + 1) / ranks);
   const float* w = p.weights + static_cast<size_t>(h) * p.cap;
   const int recent = max(p.n_first, n - p.n_recent);  // tokens from here on always stay, and those before n_first
-  const bool held = hi - lo <= SELECT_KEYS;
-  auto from_memory = [&](int i) { return select_key(w[i], i < p.n_first || i >= recent); };
-  auto key_at = [&](int i) { return held ? keys[i - lo] : from_memory(i); };
-  if (held)
-    for (int i = lo + tid; i < hi; i += SELECT_THREADS) keys[i - lo] = from_memory(i);
+  // a warp's run of tokens, 32 at a time
+  const int rounds = (hi - lo + SELECT_THREADS - 1) / SELECT_THREADS;
+  const int first = lo + warp * rounds * 32 + lane;
+  auto from_memory = [&](int j) {
+    const int i = first + 32 * j;
+    return i < hi ? select_key(w[i], i < p.n_first || i >= recent) : 0u;
+  };
+  uint32_t held[SELECT_HELD];
+  if (rounds <= SELECT_HELD) {
+    float raw[SELECT_HELD];
+#pragma unroll
+    for (int j = 0; j < SELECT_HELD; ++j) raw[j] = j < rounds && first + 32 * j < hi ? w[first + 32 * j] : 0.f;
+#pragma unroll
+    for (int j = 0; j < SELECT_HELD; ++j) {
+      const int i = first + 32 * j;
+      held[j] = i < hi ? select_key(raw[j], i < p.n_first || i >= recent) : 0u;
+    }
+  }
+  // f(j, key of token first + 32 j, whether there is one), round by round, the whole warp together
+  auto each = [&](auto&& f) {
+    if (rounds <= SELECT_HELD) {
+#pragma unroll
+      for (int j = 0; j < SELECT_HELD; ++j)
+        if (j < rounds) f(j, held[j], first + 32 * j < hi);
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < rounds; ++j) f(j, from_memory(j), first + 32 * j < hi);
+    }
+  };
 
   uint32_t prefix = 0, mask = 0, k = keep;  // the k-th largest of the keys that agree with prefix under mask
 #pragma unroll 1
   for (int digit = 0; digit < 3; ++digit) {
     const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-    uint32_t* mine = hist + (digit & 1) * SELECT_BINS;
+    uint32_t* mine = hist[digit & 1];
     for (int b = tid; b < SELECT_BINS; b += SELECT_THREADS) mine[b] = 0;
     __syncthreads();
-    for (int i0 = lo + warp * 32; i0 < hi; i0 += SELECT_THREADS) {
-      const int i = i0 + lane;
-      const uint32_t key = i < hi ? key_at(i) : 0u;
-      const bool counts_in = i < hi && (key & mask) == prefix;
-      const uint32_t bin = counts_in ? (key >> shift) & ((1u << bits) - 1u) : 0xffffffffu;
-      // lanes of one bin add once: weights crowd into few bins, and equal ones (tokens that nothing has looked at yet) into one
-      const uint32_t same = __match_any_sync(0xffffffffu, bin);
-      if (counts_in && lane == __ffs(same) - 1) atomicAdd(&mine[bin], static_cast<uint32_t>(__popc(same)));
+    each([&](int, uint32_t key, bool there) {
+      const bool counts_in = there && (key & mask) == prefix;
+      // Equal weights are common (tokens that nothing has looked at yet), and a warp of them would add to one bin 32 times in turn:
+      // the lanes that agree with the first that counts add once.
+      const uint32_t in = __ballot_sync(0xffffffffu, counts_in);
+      if (in == 0) return;
+      const uint32_t bin = (key >> shift) & ((1u << bits) - 1u);
+      const int chosen = __ffs(in) - 1;
+      const uint32_t chosen_bin = __shfl_sync(0xffffffffu, bin, chosen);  // (by every lane, also those that do not count)
+      const bool like = counts_in && bin == chosen_bin;
+      const uint32_t same = __ballot_sync(0xffffffffu, like);
+      if (lane == chosen) atomicAdd(&mine[bin], static_cast<uint32_t>(__popc(same)));
+      else if (counts_in && !like) atomicAdd(&mine[bin], 1u);
+    });
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {  // a warp sums two groups of 32 bins
+      const uint32_t sum = __reduce_add_sync(0xffffffffu, mine[(2 * warp + x) * 32 + lane]);
+      if (lane == 0) groups[digit & 1][2 * warp + x] = sum;
     }
     cluster_sync();
-    // each thread owns two bins; how many keys lie in higher bins is a suffix sum over threads
-    uint32_t c0 = 0, c1 = 0;
-    uint2 theirs[SELECT_MAX_BLOCKS];
+    // eight lanes per group, and then per bin: one for each block
+    if (tid < 8 * SELECT_GROUPS) {
+      uint32_t c = (tid & 7) < ranks ? peer_word(&groups[digit & 1][tid >> 3], tid & 7) : 0u;
 #pragma unroll
-    for (uint32_t x = 0; x < SELECT_MAX_BLOCKS; ++x) theirs[x] = x < ranks ? peer_words(&mine[2 * tid], x) : make_uint2(0, 0);
-#pragma unroll
-    for (uint32_t x = 0; x < SELECT_MAX_BLOCKS; ++x) {
-      c0 += theirs[x].x;
-      c1 += theirs[x].y;
+      for (int o = 1; o < 8; o <<= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+      if ((tid & 7) == 0) sums[tid >> 3] = c;
     }
-    uint32_t suffix = c0 + c1;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t up = __shfl_down_sync(0xffffffffu, suffix, o);
-      if (lane + o < 32) suffix += up;
-    }
-    if (lane == 0) warp_sum[warp] = suffix;
+    find_kth<SELECT_GROUPS>(sums, k, found);
+    const uint32_t group = found[0];
+    k = found[1];
     __syncthreads();
-    const uint32_t above = suffix - (c0 + c1) + __reduce_add_sync(0xffffffffu, lane > warp ? warp_sum[lane] : 0u);
-    if (above < k && k <= above + c0 + c1) {  // exactly one thread
-      const bool upper = k <= above + c1;
-      found[0] = 2 * tid + (upper ? 1 : 0);
-      found[1] = k - (upper ? above : above + c1);
+    if (tid < 8 * 32) {
+      uint32_t c = (tid & 7) < ranks ? peer_word(&mine[group * 32 + (tid >> 3)], tid & 7) : 0u;
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+      if ((tid & 7) == 0) sums[tid >> 3] = c;
     }
-    __syncthreads();
-    prefix |= found[0] << shift;
+    find_kth<32>(sums, k, found);
+    prefix |= (group * 32 + found[0]) << shift;
     mask |= ((1u << bits) - 1u) << shift;
     k = found[1];
+    __syncthreads();
   }
-  // `prefix` is the keep-th largest key, and k tokens of that key stay: the first ones.  Each warp takes a run of tokens.
-  const int per_warp = (hi - lo + 31) / 32;
-  const int a = min(hi, lo + warp * per_warp), b = min(hi, a + per_warp);
+  // `prefix` is the keep-th largest key, and k tokens of that key stay: the first ones
   uint32_t n_gt = 0, n_eq = 0;
-  for (int i0 = a; i0 < b; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t key = i < b ? key_at(i) : 0u;
-    n_gt += __popc(__ballot_sync(0xffffffffu, i < b && key > prefix));
-    n_eq += __popc(__ballot_sync(0xffffffffu, i < b && key == prefix));
-  }
+  each([&](int, uint32_t key, bool there) {
+    n_gt += __popc(__ballot_sync(0xffffffffu, there && key > prefix));
+    n_eq += __popc(__ballot_sync(0xffffffffu, there && key == prefix));
+  });
   if (lane == 0) {
     warp_gt[warp] = n_gt;
     warp_eq[warp] = n_eq;
@@ -147,25 +198,27 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
   }
   cluster_sync();
   // of the tokens before this warp's: those of the blocks before, then of the warps before
-  uint2 before_me = make_uint2(0, 0);
-  if (lane < rank) before_me = peer_words(counts, lane);
-  if (lane < warp) {
-    before_me.x += warp_gt[lane];
-    before_me.y += warp_eq[lane];
+  uint32_t gt = 0, eq = 0;
+  if (lane < rank) {
+    gt = peer_word(&counts[0], lane);
+    eq = peer_word(&counts[1], lane);
   }
-  uint32_t gt = __reduce_add_sync(0xffffffffu, before_me.x), eq = __reduce_add_sync(0xffffffffu, before_me.y);
+  if (lane < warp) {
+    gt += warp_gt[lane];
+    eq += warp_eq[lane];
+  }
+  gt = __reduce_add_sync(0xffffffffu, gt);
+  eq = __reduce_add_sync(0xffffffffu, eq);
   int32_t* out = p.index + static_cast<size_t>(h) * p.index_stride;
-  for (int i0 = a; i0 < b; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t key = i < b ? key_at(i) : 0u;
-    const bool is_gt = i < b && key > prefix, is_eq = i < b && key == prefix;
+  const uint32_t before = (1u << lane) - 1u;
+  each([&](int j, uint32_t key, bool there) {
+    const bool is_gt = there && key > prefix, is_eq = there && key == prefix;
     const uint32_t m_gt = __ballot_sync(0xffffffffu, is_gt), m_eq = __ballot_sync(0xffffffffu, is_eq);
-    const uint32_t before = (1u << lane) - 1u;
     const uint32_t my_gt = gt + __popc(m_gt & before), my_eq = eq + __popc(m_eq & before);
-    if (is_gt || (is_eq && my_eq < k)) out[my_gt + min(my_eq, k)] = i;
+    if (is_gt || (is_eq && my_eq < k)) out[my_gt + min(my_eq, k)] = first + 32 * j;
     gt += __popc(m_gt);
     eq += __popc(m_eq);
-  }
+  });
   cluster_sync();  // no block leaves while another may read its shared memory
 }
 

@@ -82,7 +82,7 @@ int enter(headcast_packed* c) {
 }
 
 // The attribute belongs to the function in a CUDA context: every cache sets it once for itself, whatever GPU it is on.
-enum { KERNEL_ROWS = 1, KERNEL_ATTN = 2, KERNEL_OBSERVE = 4, KERNEL_SELECT = 8, KERNEL_ROWS_16 = 16 };
+enum { KERNEL_ROWS = 1, KERNEL_ATTN = 2, KERNEL_OBSERVE = 4, KERNEL_ROWS_16 = 8 };
 template <typename K>
 int allow_smem(headcast_packed* c, unsigned which, K* kernel, int bytes) {
   if (c->configured & which) return HC_OK;
@@ -515,7 +515,7 @@ int64_t headcast_packed_evict_workspace_bytes(const headcast_packed* c) {
 
 int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t* keep_host, int32_t n_first, int32_t n_recent, int32_t* index,
                           int32_t index_stride, void* workspace, int64_t workspace_bytes, void* stream) {
-  int rc = enter(c);
+  const int rc = enter(c);
   if (rc != HC_OK) return rc;
   const int n_kv = c->cfg.n_kv_heads, d = c->cfg.head_dim;
   if (!to || to == c || !keep_host) return fail(c, HC_ERR_INVALID_ARG, "another cache and a number of tokens per head are needed");
@@ -549,12 +549,9 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     // blocks per head: 4096 tokens each, four a thread, keep a pass over them as short as the barriers around it
     int blocks = 1;
     while (blocks < SELECT_MAX_BLOCKS && blocks * 4096 < longest) blocks *= 2;
-    rc = allow_smem(c, KERNEL_SELECT, evict_select_kernel, SELECT_SMEM);
-    if (rc != HC_OK) return rc;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(blocks * n_kv);
     lc.blockDim = dim3(SELECT_THREADS);
-    lc.dynamicSmemBytes = SELECT_SMEM;
     lc.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
