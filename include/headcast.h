@@ -383,8 +383,8 @@ int64_t headcast_packed_evict_workspace_bytes(const headcast_packed* cache);
 int headcast_packed_evict(headcast_packed* cache, headcast_packed* to, const int32_t* keep_host, int32_t n_first, int32_t n_recent, int32_t* index_dev,
                           int32_t index_stride, void* workspace_dev, int64_t workspace_bytes, void* stream);
 
-/* Synchronises `stream` and reports whether a kernel of this cache gave up on a bounded wait (HC_ERR_TIMEOUT; later launches
- * compute nothing until it is reported). */
+/* Synchronises `stream` and reports whether a kernel of this cache gave up on a bounded wait (HC_ERR_TIMEOUT: the outputs of that
+ * call, and of the attends and observes after it up to this report, are undefined). */
 int headcast_packed_check(headcast_packed* cache, void* stream);
 const char* headcast_packed_last_error(const headcast_packed* cache);
 

@@ -125,30 +125,27 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
       mbar_init(&bar_kv_full[s], 4);
       mbar_init(&bar_kv_free[s], 1);
     }
+    abort_flag = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
     tmem_alloc(&tmem_slot, TMEM_COLS);
     tmem_relinquish();
   }
-  pdl_launch_dependents();
-  pdl_wait();
-  if (tid == 0) abort_flag = (*reinterpret_cast<volatile int32_t*>(p.c.status) != 0) ? 1 : 0;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  // All of the above runs while the kernel before drains.
+  pdl_launch_dependents();
+  pdl_wait();
   const uint32_t tmem = tmem_slot;
   volatile int* abortp = &abort_flag;
-  const bool dead_on_arrival = abort_flag != 0;  // a kernel gave up and the host has not heard of it yet
-  __syncthreads();                               // (the flag is read before any wait can raise it)
   const int64_t total = p.line_first[p.c.n_kv];
   const int64_t x_lo = share_begin(blockIdx.x, total, p.n_cta), x_hi = share_begin(blockIdx.x + 1, total, p.n_cta);
   int64_t x = x_lo;
   int head = 0;
 
-  if (dead_on_arrival) {
-    // nothing: straight to the teardown
-  } else if (warp < 4) {
+  if (warp < 4) {
     regs_dec<PATTN_REGS_ISSUE>();
     if (warp == 0) {
       // ---------------------------------------------------------------- MMA issuer (the whole warp, converged)

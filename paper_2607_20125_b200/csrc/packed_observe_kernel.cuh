@@ -88,31 +88,28 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
       mbar_init(&bar_l_full[i], 2);
       mbar_init(&bar_l_free[i], 16);
     }
+    abort_flag = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
     tmem_alloc(&tmem_slot, TMEM_COLS);
     tmem_relinquish();
   }
-  pdl_launch_dependents();
-  pdl_wait();
-  if (tid == 0) abort_flag = (*reinterpret_cast<volatile int32_t*>(p.c.status) != 0) ? 1 : 0;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  // All of the above runs while the kernel before drains.
+  pdl_launch_dependents();
+  pdl_wait();
   const uint32_t tmem = tmem_slot;
   volatile int* abortp = &abort_flag;
-  const bool dead_on_arrival = abort_flag != 0;
-  __syncthreads();
   const int64_t total = p.line_first[p.c.n_kv];
   int64_t x = share_begin(blockIdx.x, total, p.n_cta);
   const int64_t x_hi = share_begin(blockIdx.x + 1, total, p.n_cta);
   int head = 0;
   float* const lse_ring = reinterpret_cast<float*>(smem + SM::LSE_OFF);
 
-  if (dead_on_arrival) {
-    // nothing: straight to the teardown
-  } else if (warp == 0) {
+  if (warp == 0) {
     // ------------------------------------------------------------------ products (the whole warp, converged)
     const uint32_t elected = elect_one();
     const uint32_t idesc = idesc_bf16_f32(128, 128, 0, 0);

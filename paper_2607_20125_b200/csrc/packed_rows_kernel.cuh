@@ -128,14 +128,13 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
       mbar_init(&bar_full[s], 1);
       done[s] = loads[s] = 0;
     }
+    abort_flag = 0;
     fence_mbar_init();
   }
   pdl_launch_dependents();
   pdl_wait();
   if (tid == 0)
     for (int i = 0; i < min(t_hi - t_lo, SM::STAGES); ++i) load_tile(i, head);
-  // a kernel that gave up and of which the host has not heard: nothing is computed (the flag is seen behind the first barrier)
-  if (tid == WARPS * 32 - 1) abort_flag = *reinterpret_cast<volatile int32_t*>(p.c.status) != 0;
   volatile int* abortp = &abort_flag;
   const int group = warp / ROWS_GROUP_WARPS, key0 = (warp % ROWS_GROUP_WARPS) * 16;
   const int r = lane >> 2, q = lane & 3;
@@ -155,7 +154,6 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
       stage_row<D>(qs, row_scale, p.q + (static_cast<size_t>(token) * (p.c.n_kv * p.group) + h) * D, warp, warp < p.n_rows, p.scale_log2e);
     }
     __syncthreads();
-    if (t0 == t_lo) ok = abort_flag == 0;
     float c[NQ][2], m[NQ][2], l[NQ][2];  // of this lane's two queries per tile: columns 2q and 2q + 1
     float o[NQ][NT][4];
 #pragma unroll

@@ -28,7 +28,7 @@ constexpr int ROPE_THREADS = 256;
 // HALVES: pairs are (i, i + pairs) instead of (2i, 2i + 1).
 // TOKENS per block: a power of two that leaves enough blocks (chosen by the caller).
 template <int D, bool HALVES>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeParams p, int tokens_per_block) {
+__global__ void __launch_bounds__(ROPE_THREADS, 8) rope_kernel(const __grid_constant__ RopeParams p, int tokens_per_block) {
   extern __shared__ float2 turn[];  // [tokens_per_block][D / 2] cosine and sine
   constexpr int PAIRS = D / 2;
   pdl_launch_dependents();

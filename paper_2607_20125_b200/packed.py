@@ -164,6 +164,7 @@ class PackedCache:
         if rc != 0:
             self._ptr = C.c_void_p()
             raise HeadCastError(rc, "headcast_packed_create failed")
+        self._lengths = (C.c_int32 * self.n_kv_heads)()
         stride = C.c_int64()
         at = self.lib.headcast_packed_weights_offset(self._ptr, C.byref(stride))
         self._weights = self.storage[at:at + 4 * stride.value * self.n_kv_heads].view(torch.float32).view(self.n_kv_heads, stride.value)
@@ -192,11 +193,10 @@ class PackedCache:
 
     def lengths(self):
         """Tokens per key/value head."""
-        arr = (C.c_int32 * self.n_kv_heads)()
-        rc = self.lib.headcast_packed_lengths(self._ptr, arr)
+        rc = self.lib.headcast_packed_lengths(self._ptr, self._lengths)
         if rc != 0:
             self._raise(rc)
-        return list(arr)
+        return self._lengths[:]
 
     def clear(self) -> None:
         rc = self.lib.headcast_packed_clear(self._ptr)
