@@ -52,6 +52,12 @@ int fail(headcast_packed* c, int code, const char* fmt, ...) {
 
 bool aligned(const void* p, uintptr_t to = 16) { return p && reinterpret_cast<uintptr_t>(p) % to == 0; }
 
+// [a, a + bytes_a) and [b, b + bytes_b) share a byte
+bool overlap(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + static_cast<uintptr_t>(bytes_b) && y < x + static_cast<uintptr_t>(bytes_a);
+}
+
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 bool config_ok(const headcast_packed_config* cfg) {
@@ -211,12 +217,6 @@ thread_local char g_rope_error[256] = "";
 int rope_fail(int code, const char* msg) {
   snprintf(g_rope_error, sizeof(g_rope_error), "%s", msg);
   return code;
-}
-
-// [a, a + bytes_a) and [b, b + bytes_b) share a byte
-bool overlap(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + static_cast<uintptr_t>(bytes_b) && y < x + static_cast<uintptr_t>(bytes_a);
 }
 
 }  // namespace
@@ -453,6 +453,8 @@ int headcast_packed_attend(headcast_packed* c, const void* q, void* out, float* 
   if (n_queries < 0 || static_cast<int64_t>(n_queries) * c->cfg.n_heads > INT32_MAX - 512) return fail(c, HC_ERR_INVALID_ARG, "n_queries out of range");
   if (n_queries == 0) return HC_OK;
   if (!aligned(q) || !aligned(out)) return fail(c, HC_ERR_INVALID_ARG, "q and out must be 16-byte aligned device pointers");
+  const int64_t q_bytes = 2ll * n_queries * c->cfg.n_heads * c->cfg.head_dim;
+  if (q != out && overlap(q, q_bytes, out, q_bytes)) return fail(c, HC_ERR_INVALID_ARG, "out overlaps q without being q");
   if (lse && !aligned(lse, 4)) return fail(c, HC_ERR_INVALID_ARG, "lse must be 4-byte aligned");
   if (!aligned(workspace, 256) || workspace_bytes < headcast_packed_workspace_bytes(c, n_queries))
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_workspace_bytes(%d)", n_queries);

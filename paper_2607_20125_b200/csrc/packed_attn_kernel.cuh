@@ -360,6 +360,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
               for (int i = 0; i < 32; i += 2) mx = max3(mx, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
             }
             mx *= c;
+            if (beyond_limit(mx)) c = __uint_as_float(0x7fffffffu);
             if (__any_sync(0xffffffffu, mx > m_ref + P_HEADROOM + 1.f)) {
               const float m_new = mx > m_ref + P_HEADROOM ? mx - P_HEADROOM : m_ref;
               const float alpha = ex2_approx(m_ref - m_new);

@@ -127,6 +127,9 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 constexpr float P_HEADROOM = 6.f, P_LAG = 14.f;
 // The reference of a row that has met no logit yet (or only NaNs): below all of them, and finite, so that exponentials need no case for it.
 constexpr float NO_REFERENCE = -3e38f;
+// From here on (log2 domain) a reference in fp32 may be further from the largest logit than its exponential can stand: the row becomes NaN.
+constexpr float LOGIT_LIMIT = 4194304.f;
+__device__ __forceinline__ bool beyond_limit(float mx) { return fabsf(mx) >= LOGIT_LIMIT && mx != -INFINITY; }
 
 // The factor that brings a query row whose largest magnitude is `amax` to magnitudes below 2^15, and its inverse: powers of two, so
 // every element of a bf16 row that is not smaller than 2^-28 of the largest is exact in fp16, and the others are off by

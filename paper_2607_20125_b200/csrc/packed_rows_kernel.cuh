@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
             mx *= c[z][y];
+            if (beyond_limit(mx)) c[z][y] = __uint_as_float(0x7fffffffu);
             const float to = mx > m[z][y] + P_HEADROOM ? mx - P_HEADROOM : m[z][y];
             const float f = ex2_approx(m[z][y] - to);
             m[z][y] = to;

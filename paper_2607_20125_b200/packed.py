@@ -8,6 +8,7 @@ current device; work runs on the current torch stream.  There is no fallback: a 
 from __future__ import annotations
 
 import ctypes as C
+import operator
 from typing import Optional, Sequence, Union
 
 import torch
@@ -103,6 +104,14 @@ def _rows(t, name: str, shape, device: int):
     return t.data_ptr(), stride
 
 
+def _int(value, name: str, bits: int = 32) -> int:
+    """ctypes would cut a number that is too large down to one that is not."""
+    value = operator.index(value)
+    if not -(1 << (bits - 1)) <= value < 1 << (bits - 1):
+        raise ValueError(f"{name}: {value} is out of range")
+    return value
+
+
 def _count(t) -> int:
     """Tokens of a [tokens, heads, d] tensor; -1, which no shape matches, for anything else."""
     return t.shape[0] if isinstance(t, torch.Tensor) and t.dim() == 3 else -1
@@ -118,9 +127,10 @@ class Rope:
             dims = (head_dim - 4 * (head_dim // 6), 2 * (head_dim // 6), 2 * (head_dim // 6))
         cfg = RopeConfig()
         self.lib.headcast_rope_default_config(C.byref(cfg))
-        cfg.n_heads, cfg.n_kv_heads, cfg.head_dim = n_heads, n_heads if n_kv_heads is None else n_kv_heads, head_dim
-        cfg.grid_h, cfg.grid_w, cfg.halves, cfg.theta = grid_h, grid_w, int(halves), theta
-        cfg.dim_t, cfg.dim_h, cfg.dim_w = dims
+        cfg.n_heads, cfg.n_kv_heads = _int(n_heads, "n_heads"), _int(n_heads if n_kv_heads is None else n_kv_heads, "n_kv_heads")
+        cfg.head_dim, cfg.grid_h, cfg.grid_w = _int(head_dim, "head_dim"), _int(grid_h, "grid_h"), _int(grid_w, "grid_w")
+        cfg.halves, cfg.theta = bool(halves), theta
+        cfg.dim_t, cfg.dim_h, cfg.dim_w = (_int(v, "dims") for v in dims)
         cfg.scale_t, cfg.scale_h, cfg.scale_w = scales
         self.cfg, self._cfg = cfg, C.byref(cfg)
 
@@ -138,21 +148,22 @@ class Rope:
             k_ptr, k_stride = _rows(k, "k", shape, device)
             k_out_ptr = _tensor(k_out, "k_out", shape, torch.bfloat16, device)
         pos = None if positions is None else _tensor(positions, "positions", (n, 3), torch.int32, device)
-        rc = self.lib.headcast_rope(self._cfg, q_ptr, q_out_ptr, q_stride, k_ptr, k_out_ptr, k_stride, n, first_frame, pos, inverse, _raw_stream(device))
+        rc = self.lib.headcast_rope(self._cfg, q_ptr, q_out_ptr, q_stride, k_ptr, k_out_ptr, k_stride, n, _int(first_frame, "first_frame", 64), pos, bool(inverse), _raw_stream(device))
         if rc != 0:
             raise HeadCastError(rc, self.lib.headcast_rope_last_error().decode())
 
 
 class PackedCache:
-    """One layer's key/value cache in 4 bits (wraps headcast_packed*).  The storage is a torch tensor of the current device; every
-    call takes its workspace from torch's allocator on the current stream, so calls and captured graphs share none."""
+    """One layer's key/value cache in 4 bits (wraps headcast_packed*).  The storage is a torch tensor of the current device and stream
+    (keep the cache until work on other streams is done); every call takes its workspace from torch's allocator on the current
+    stream, so calls and captured graphs share none."""
 
     def __init__(self, n_heads: int, head_dim: int, capacity: int, n_kv_heads: Optional[int] = None, softmax_scale: float = 0.0):
         self._ptr = C.c_void_p()
         self.lib = load_library()
         self.n_heads, self.head_dim, self.capacity = n_heads, head_dim, capacity
         self.n_kv_heads = n_heads if n_kv_heads is None else n_kv_heads
-        self.cfg = PackedConfig(n_heads, self.n_kv_heads, head_dim, capacity, softmax_scale)
+        self.cfg = PackedConfig(_int(n_heads, "n_heads"), _int(self.n_kv_heads, "n_kv_heads"), _int(head_dim, "head_dim"), _int(capacity, "capacity"), softmax_scale)
         size = self.lib.headcast_packed_bytes(C.byref(self.cfg))
         if size < 0:
             raise HeadCastError(size, "sizes out of range (1..64 heads, a divisor of them for keys and values, head_dim 64 or 128, capacity 1..2^23, "
@@ -204,7 +215,7 @@ class PackedCache:
             self._raise(rc)
 
     def drop_last(self, n_tokens: int) -> None:
-        rc = self.lib.headcast_packed_drop_last(self._ptr, n_tokens)
+        rc = self.lib.headcast_packed_drop_last(self._ptr, _int(n_tokens, "n_tokens"))
         if rc != 0:
             self._raise(rc)
 
@@ -222,8 +233,8 @@ class PackedCache:
 
     def export(self, first: int = 0, n_tokens: Optional[int] = None):
         """(K, V) bf16 [n_kv_heads, n, d]: the held values, zeros where a head has no token."""
-        lengths = self.lengths()
-        n = max(0, max(lengths) - first) if n_tokens is None else n_tokens
+        lengths, first = self.lengths(), _int(first, "first")
+        n = max(0, max(lengths) - first) if n_tokens is None else _int(n_tokens, "n_tokens")
         if n < 0:
             raise ValueError(f"n_tokens must not be negative, got {n}")
         make = torch.empty if first + n <= min(lengths) else torch.zeros
@@ -263,7 +274,7 @@ class PackedCache:
         largest weights besides, ``keep`` tokens in all (one number, or one per key/value head; a shorter head moves whole).  index:
         int32 [n_kv_heads, >= longest result] or None, receives the places that the tokens had."""
         lib, kv, device = self.lib, self.n_kv_heads, self._device
-        keep = [keep] * kv if isinstance(keep, int) else [int(v) for v in keep]
+        keep = [_int(keep, "keep")] * kv if hasattr(keep, "__index__") else [_int(v, "keep") for v in keep]
         if len(keep) != kv:
             raise ValueError(f"keep: expected {kv} entries, got {len(keep)}")
         if not isinstance(other, PackedCache) or not other._ptr:
@@ -275,7 +286,7 @@ class PackedCache:
         else:
             size = lib.headcast_packed_evict_workspace_bytes(self._ptr)
             ws = self._workspace(size)
-        rc = lib.headcast_packed_evict(self._ptr, other._ptr, (C.c_int32 * kv)(*keep), n_first, n_recent, ptr, width, None if ws is None else ws.data_ptr(), size,
+        rc = lib.headcast_packed_evict(self._ptr, other._ptr, (C.c_int32 * kv)(*keep), _int(n_first, "n_first"), _int(n_recent, "n_recent"), ptr, width, None if ws is None else ws.data_ptr(), size,
                                        _raw_stream(device))
         if rc != 0:
             self._raise(rc)

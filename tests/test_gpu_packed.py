@@ -186,6 +186,100 @@ def test_rows_of_any_size_and_rows_that_are_not_finite(n_q):
     assert torch.equal(out[~rows], good[~rows]) and torch.equal(lse.T[~rows], good_lse.T[~rows])
 
 
+@pytest.mark.parametrize("n_q", [2, 150])
+def test_logits_of_any_size(n_q):
+    """Up to the limit rows are as exact as their logits; a row beyond it is NaN, whichever way its logits point, and no other."""
+    import torch
+    g = gen(14)
+    n, d = 700, 64
+    k, v, q = randn(g, n, 2, d), randn(g, n, 2, d), randn(g, n_q, 2, d)
+    hk, hv = per_head(k), per_head(v)
+    for scale in (2.0 ** -30, 1.0, 2.0 ** 10):
+        cache = make(2, 2, d, n, k, v, softmax_scale=scale)
+        out, lse = attend(cache, q)
+        ref.check_attend(out, lse, q, hk, hv, scale)
+    cache = make(2, 2, d, n, k, v, softmax_scale=1.0)
+    far = q.clone()
+    far[0, 0] *= 1e9
+    near, near_lse = attend(cache, q)
+    out, lse = attend(cache, far)
+    assert torch.isnan(out[0, 0].float()).all() and torch.isnan(lse[0, 0])
+    assert torch.equal(out[1:], near[1:]) and torch.equal(out[:, 1], near[:, 1]) and torch.equal(lse[1], near_lse[1])
+    down = make(2, 2, d, n, k.abs(), v, softmax_scale=1.0)
+    far[0, 0] = -far[0, 0].abs()
+    out, lse = attend(down, far)
+    assert torch.isnan(out[0, 0].float()).all() and torch.isfinite(out[1:].float()).all()
+
+
+@pytest.mark.parametrize("n_q", [3, 150, 700])
+def test_output_in_place_of_the_queries(n_q):
+    import torch
+    from paper_2607_20125_b200.binding import HeadCastError
+    g = gen(15)
+    k, v, q = randn(g, 3000, 2, 128), randn(g, 3000, 2, 128), randn(g, n_q + 1, 4, 128)
+    cache = make(4, 2, 128, 3000, k, v)
+    out, lse = attend(cache, q[:n_q])
+    both = q.clone()
+    again = torch.empty_like(lse)
+    cache.attend(both[:n_q], both[:n_q], again)
+    assert torch.equal(both[:n_q], out) and torch.equal(again, lse) and torch.equal(both[n_q:], q[n_q:])
+    with pytest.raises(HeadCastError) as e:
+        cache.attend(both[:n_q], both[1:], again)
+    assert e.value.code == -1
+
+
+@pytest.mark.parametrize("n_q", [3, 700])
+def test_a_kernel_that_gave_up_is_reported_once(n_q):
+    """As if a bounded wait of an earlier call had expired: its status word stands in the storage."""
+    import torch
+    from paper_2607_20125_b200.binding import HeadCastError
+    g = gen(16)
+    k, v, q = randn(g, 3000, 2, 128), randn(g, 3000, 2, 128), randn(g, n_q, 2, 128)
+    cache = make(2, 2, 128, 3000, k, v)
+    out, lse = attend(cache, q)
+    cache.storage[:4].view(torch.int32).fill_(77)
+    cache.attend(q, torch.empty_like(q), torch.empty_like(lse))
+    with pytest.raises(HeadCastError) as e:
+        cache.check()
+    assert e.value.code == -6 and "77" in str(e.value)
+    cache.check()
+    again, again_lse = attend(cache, q)
+    assert torch.equal(again, out) and torch.equal(again_lse, lse)
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2607_20125_b200.packed import PackedCache, Rope
+caches = [PackedCache(2, 64, 600) for _ in range(2)]
+k, v, q, one = (torch.randn(n, 2, 64, device="cuda").bfloat16() for n in (500, 500, 300, 1))
+outs = [torch.empty_like(q), torch.empty(2, 300, device="cuda"), torch.empty_like(one), torch.empty(2, 1, device="cuda")]
+def calls():
+    Rope(2, 64, 10, 10, dims=(24, 20, 20)).apply(q, outs[0])
+    caches[0].clear()
+    caches[0].append(k, v)
+    caches[0].attend(q, outs[0], outs[1])
+    caches[0].attend(one, outs[2], outs[3])
+    caches[0].observe(q, outs[1], decay=0.0)
+    caches[0].evict_into(caches[1], 200)
+    return [o.clone() for o in outs] + [caches[0].weights.clone()] + list(caches[1].export())
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    captured = calls()
+graph.replay()
+torch.cuda.synchronize()
+captured = [c.clone() for c in captured]
+assert all(torch.equal(a, b) for a, b in zip(captured, calls()))
+print("same")
+"""
+    import os
+    res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=200, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert res.returncode == 0 and "same" in res.stdout, res.stdout + res.stderr
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n_q", [5, 200])
 def test_row_maximum_grows_and_falls(d, n_q):
@@ -491,6 +585,10 @@ def test_refusals_leave_the_cache_as_it_was():
                 lambda: cache.attend(q.transpose(0, 1), torch.empty_like(q)), lambda: cache.attend(q, torch.empty_like(q), torch.empty(5, 4, device="cuda")),
                 lambda: cache.attend(q.cpu(), torch.empty_like(q)), lambda: cache.observe(q, torch.empty(4, 6, device="cuda")),
                 lambda: cache.evict_into(cache, [1]), lambda: cache.evict_into(None, 1)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: cache.drop_last(1 << 32), lambda: cache.export(first=1 << 33), lambda: cache.evict_into(make(4, 2, 64, 90), (1 << 32) + 5),
+                lambda: make(4, 2, 64, (1 << 32) + 100)):  # numbers that ctypes would cut down to valid ones
         with pytest.raises(ValueError):
             bad()
     for bad, code in ((lambda: cache.evict_into(cache, 10), -1), (lambda: cache.evict_into(make(4, 2, 64, 9), 10), -2), (lambda: cache.evict_into(make(2, 2, 128, 90), 10), -1),

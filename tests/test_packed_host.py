@@ -123,6 +123,7 @@ def test_refusals():
         (lambda: c.export(0, 5, PTR + 8, PTR, None), "aligned"),
         (lambda: c.attend(PTR, PTR, None, -1, PTR, ws, None), "range"), (lambda: c.attend(PTR, PTR, None, 1 << 30, PTR, ws, None), "range"),
         (lambda: c.attend(None, PTR, None, 8, PTR, ws, None), "aligned"), (lambda: c.attend(PTR, PTR + 8, None, 8, PTR, ws, None), "aligned"),
+        (lambda: c.attend(PTR, PTR + 512, None, 8, PTR, ws, None), "overlaps"),
         (lambda: c.attend(PTR, PTR, C.c_void_p(PTR + 2), 8, PTR, ws, None), "aligned"),
         (lambda: c.attend(PTR, PTR, None, 8, PTR, ws - 1, None), "workspace"), (lambda: c.attend(PTR, PTR, None, 9, PTR, ws, None), "workspace"),
         (lambda: c.attend(PTR, PTR, None, 8, PTR + 16, ws, None), "workspace"), (lambda: c.attend(PTR, PTR, None, 8, None, ws, None), "workspace"),
