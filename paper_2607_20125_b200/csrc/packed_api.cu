@@ -114,6 +114,8 @@ T step_line(const headcast_packed* c, T (&first)[PACK_MAX_HEADS + 1], T per_tile
   return total;
 }
 
+// Up to 16 rows per key/value head go to packed_rows_kernel: 16 x 32760 tokens, 12 heads of 128, 28 us; packed_attn_kernel, for which
+// 17 rows are as much work as 128, takes 48.
 bool few_rows(const headcast_packed* c, int32_t n_queries) { return static_cast<int64_t>(n_queries) * (c->cfg.n_heads / c->cfg.n_kv_heads) <= ROWS_MAX; }
 
 struct RowsWorkspace {
@@ -145,7 +147,7 @@ int attend_few(headcast_packed* c, const void* q, void* out, float* lse, int32_t
   const int total = step_line(c, p.tile_first, 1);
   p.n_cta = std::min(c->n_sm, total);
   if (total > 0) {
-    const bool one = p.n_rows <= 8;
+    const bool one = p.n_rows <= 8;  // 32760 tokens, 12 heads of 128: 21.4 us; with two tiles of queries 28.3
     const int smem = RowsSmem<D>::DYN_BYTES;
     auto* kernel = one ? packed_rows_kernel<D, 1> : packed_rows_kernel<D, 2>;
     const int rc = allow_smem(c, one ? KERNEL_ROWS : KERNEL_ROWS_16, kernel, smem);
@@ -200,7 +202,10 @@ int attend_many(headcast_packed* c, const void* q, void* out, float* lse, int32_
       int64_t pairs = 0;
       for (int h = 0; h < c->cfg.n_kv_heads; ++h) pairs += c->len[h] > 0 ? p.n_pairs : 0;
       const bool by_pair = pairs < p.n_cta - 1;
-      const int groups = parts <= 4 ? 1 : parts <= 24 ? 4 : 16;
+      // Groups of threads that share a row's parts: with one 57 us for 700 queries x 9000 tokens (6 parts a pair; with four 65, with sixteen
+      // 94), with four 23.8 us for 77 x 10007, 16 / 4 heads of 64 (20 parts; 26.5 and 25.4), with sixteen 23 us for 200 x 25000, one head
+      // (148 parts; 78 and 36).
+      const int groups = parts <= 10 ? 1 : parts <= 24 ? 4 : 16;
       auto* merge = groups == 1 ? packed_merge_kernel<D, 1> : groups == 4 ? packed_merge_kernel<D, 4> : packed_merge_kernel<D, 16>;
       PK_CUDA(c, launch_pdl(merge, dim3((by_pair ? static_cast<int>(pairs) : p.n_cta - 1) * 16 * groups), dim3(16 * D / 8), 0, st, p, by_pair));
     }
@@ -299,7 +304,8 @@ int headcast_rope(const headcast_rope_config* cfg, const void* q, void* q_out, i
       p.frequency[i] = inverse ? 0 - f : f;
     }
   }
-  // tokens of a block: as many as leave every SM a few blocks, at most 8 (their sines and cosines are formed once for all heads)
+  // Tokens of a block (their sines and cosines are formed once for all heads): 8 where every SM gets a few blocks (a 68 x 120 block 56.4 us;
+  // 4 tokens 57.0, 16 61.4), fewer in small calls.
   int per_block = 8;
   while (per_block > 1 && (n_tokens + per_block - 1) / per_block < 148 * 4) per_block /= 2;
   const dim3 grid((n_tokens + per_block - 1) / per_block);
@@ -548,7 +554,8 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     s.cap = c->view.cap;
     s.n_first = n_first;
     s.n_recent = n_recent;
-    // blocks per head: 4096 tokens each, four a thread, keep a pass over them as short as the barriers around it
+    // Blocks per head, 4096 tokens each: 1000 tokens 10.8 us with one block and 12.4 with eight, 9000 17.8 / 15.0 (four), 75600 189 / 46.8
+    // (eight; selection and move, 12 heads of 128).
     int blocks = 1;
     while (blocks < SELECT_MAX_BLOCKS && blocks * 4096 < longest) blocks *= 2;
     cudaLaunchConfig_t lc = {};

@@ -14,6 +14,10 @@
 // The steps (one tile for both query tiles) of all items are laid end to end and every CTA, one per SM, takes an equal share; an
 // item that is cut leaves partial results that packed_merge_kernel joins.  No lists: every role finds its items by division.
 // The packed streams are 3.6 times smaller than bf16, so they share L2 where bf16 streams had to be taken in turn.
+//
+// What bounds it: a tile's softmax (1700 clk alone on its schedulers, 2000 beside the other tile's) and its products (1024, and 350 until
+// their results are seen) follow one another; two tiles overlap to 3700 clk a step.  4680 queries x 32760 tokens, 12 heads of 128: 730 us,
+// 1290 TFLOP/s, and at the power cap up to 850; 10800 x 75600: 4.35 ms.
 #pragma once
 #include "packed_format.cuh"
 

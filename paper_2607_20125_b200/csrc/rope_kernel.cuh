@@ -3,7 +3,7 @@
 // The angle is formed in turns, in 64-bit integers: a frequency is a fraction of a turn per position in units of 2^-64 turn, and
 // position * frequency modulo 2^64 is the exact fractional turn, for positions of any size and sign.  Its upper 32 bits go
 // to sincospif, so that a far position is as exact as a near one (an angle of 10^5 in fp32 is off by 4e-3).
-// Bound by memory: every value is read and written once, 4 bytes together.  A block forms the sines and cosines of its tokens once,
+// Bound by memory: every value is read and written once, 4 bytes together; 24480 tokens of 12 + 12 heads of 128 in 54 us, 5.5 TB/s.  A block forms the sines and cosines of its tokens once,
 // in shared memory, for all heads of queries and keys.
 #pragma once
 #include "tc05.cuh"
