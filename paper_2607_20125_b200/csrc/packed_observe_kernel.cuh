@@ -283,6 +283,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
           sum += a0 + a1;
         }
         tc_fence_before_sync();
+        __threadfence_block();  // the log-sum-exps have been read, not only asked for, when their slot is given back
         __syncwarp();
         mbar_arrive_if(&bar_s_free[buf], lane == 0);
         mbar_arrive_if(&bar_l_free[st], lane == 0);
