@@ -493,6 +493,26 @@ int headcast_packed_observe(headcast_packed* c, const void* q, const float* lse,
   if (!aligned(lse, 4)) return fail(c, HC_ERR_INVALID_ARG, "lse must be a 4-byte aligned device pointer");
   if (!aligned(workspace, 256) || workspace_bytes < headcast_packed_workspace_bytes(c, n_queries))
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_workspace_bytes(%d)", n_queries);
+  if (few_rows(c, n_queries)) {
+    PackedObserveRowsParams r;
+    std::memset(&r, 0, sizeof(r));
+    r.c = c->view;
+    r.q = static_cast<const __nv_bfloat16*>(q);
+    r.lse = lse;
+    r.n_queries = n_queries;
+    r.group = c->cfg.n_heads / c->cfg.n_kv_heads;
+    r.n_rows = n_queries * r.group;
+    r.scale_log2e = c->scale * 1.4426950408889634f;
+    r.decay = decay;
+    r.len = p.len;
+    // four blocks per SM, as many for every head
+    const int tiles = (longest + PACK_TILE - 1) / PACK_TILE, blocks = std::min(tiles, std::max(1, 4 * c->n_sm / c->cfg.n_kv_heads));
+    const bool one = r.n_rows <= 8;
+    auto* rows_kernel = c->cfg.head_dim == 128 ? (one ? packed_observe_rows_kernel<128, 1> : packed_observe_rows_kernel<128, 2>)
+                                               : (one ? packed_observe_rows_kernel<64, 1> : packed_observe_rows_kernel<64, 2>);
+    PK_CUDA(c, launch_pdl(rows_kernel, dim3(blocks, c->cfg.n_kv_heads), dim3(OBSERVE_ROWS_THREADS), 0, st, r));
+    return HC_OK;
+  }
   p.lse = lse;
   p.part = static_cast<float*>(workspace);
   p.n_queries = n_queries;

@@ -434,4 +434,108 @@ __global__ void __launch_bounds__(MERGE_GROUPS * D / 4) packed_merge_rows_kernel
   if (p.lse && c == 0) p.lse[static_cast<size_t>(h) * p.n_queries + token] = n == 0 ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
+// What up to 16 query rows per key/value head give to every token: weight = decay * weight + sum over the rows of exp(logit - lse).
+// The products are those of packed_rows_kernel without the values; a row of S^T is a token and its columns the queries, so a
+// token's sum is four lanes' to add and each token belongs to one warp: no parts, no second kernel.  Keys are read straight into registers, a
+// tile ahead; 73 bytes per token and head at d = 128.  One query, 32760 tokens, 12 heads of 128: OBS_ROWS_US us (packed_observe_kernel, for
+// which one query is as much work as 32: 32).
+struct PackedObserveRowsParams {
+  PackedView c;
+  const __nv_bfloat16* q;
+  const float* lse;  // [n_kv * group][n_queries]
+  int32_t n_queries, group, n_rows;
+  float scale_log2e, decay;
+  HeadCounts len;
+};
+constexpr int OBSERVE_ROWS_THREADS = 256;
+
+template <int D, int NQ>
+__global__ void __launch_bounds__(OBSERVE_ROWS_THREADS) packed_observe_rows_kernel(const __grid_constant__ PackedObserveRowsParams p) {
+  constexpr int KW = D / 32, WARPS = OBSERVE_ROWS_THREADS / 32;
+  __shared__ uint2 qs[D / 16 * 2 * 32];
+  __shared__ float row_scale[ROWS_MAX], row_lse[ROWS_MAX];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3, head = blockIdx.y;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int len = p.len.n[head], tiles = (len + PACK_TILE - 1) / PACK_TILE;
+  if (static_cast<int>(blockIdx.x) >= tiles) return;
+  const size_t row0 = static_cast<size_t>(head) * p.c.cap + warp * 16 + r;  // of this lane's first token in tile 0; the second is 8 rows on
+  struct Keys {
+    uint32_t w[2][KW], scales[2];
+  };
+  auto fetch = [&](Keys& k, int tile) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const size_t row = row0 + static_cast<size_t>(tile) * PACK_TILE + 8 * j;
+      if (D == 128) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p.c.k_codes + row * (D / 2) + q * 16);
+        k.w[j][0] = v.x; k.w[j][1] = v.y; k.w[j][KW - 2] = v.z; k.w[j][KW - 1] = v.w;
+        k.scales[j] = *reinterpret_cast<const uint16_t*>(p.c.k_scales + row * (D / PACK_GROUP) + q * 2);
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(p.c.k_codes + row * (D / 2) + q * 8);
+        k.w[j][0] = v.x; k.w[j][1] = v.y;
+        k.scales[j] = p.c.k_scales[row * (D / PACK_GROUP) + q];
+      }
+    }
+  };
+  Keys next;
+  fetch(next, blockIdx.x);
+  for (int i = warp; i < 8 * NQ; i += WARPS) {
+    const int token = i / p.group, h = head * p.group + i % p.group;
+    const bool valid = i < p.n_rows;
+    stage_row<D>(qs, row_scale, p.q + (static_cast<size_t>(token) * (p.c.n_kv * p.group) + h) * D, i, valid, p.scale_log2e);
+    if (lane == 0) row_lse[i] = valid ? -1.4426950408889634f * p.lse[static_cast<size_t>(h) * p.n_queries + token] : -INFINITY;
+  }
+  __syncthreads();
+  float c[NQ][2], l[NQ][2];  // of this lane's two queries per tile: columns 2q and 2q + 1
+#pragma unroll
+  for (int z = 0; z < NQ; ++z)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      c[z][y] = row_scale[8 * z + 2 * q + y];
+      l[z][y] = row_lse[8 * z + 2 * q + y];
+    }
+  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const Keys k = next;
+    if (tile + static_cast<int>(gridDim.x) < tiles) fetch(next, tile + gridDim.x);
+    float s[NQ][4], s_odd[NQ][4];
+#pragma unroll
+    for (int z = 0; z < NQ; ++z)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) s[z][y] = s_odd[z][y] = 0.f;
+#pragma unroll
+    for (int x = 0; x < KW; ++x) {
+      uint32_t a[2][4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t sc = scale_f16x2(k.scales[j], x / 2);
+        codes_to_f16x2(k.w[j][x], a[j]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) a[j][y] = mul_f16x2(a[j][y], sc);
+      }
+#pragma unroll
+      for (int z = 0; z < NQ; ++z) {
+        const uint2 b0 = qs[(4 * x + z) * 32 + lane], b1 = qs[(4 * x + 2 + z) * 32 + lane];
+        mma_16816(s[z], a[0][0], a[1][0], a[0][1], a[1][1], b0.x, b0.y);
+        mma_16816(s_odd[z], a[0][2], a[1][2], a[0][3], a[1][3], b1.x, b1.y);
+      }
+    }
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int z = 0; z < NQ; ++z)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) sum[y / 2] += ex2_approx(fmaf(s[z][y] + s_odd[z][y], c[z][y & 1], l[z][y & 1]));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
+      sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+    }
+    const int token = tile * PACK_TILE + warp * 16 + r + 8 * q;  // lane q = 0 writes the first token, q = 1 the second
+    if (q < 2 && token < len) {
+      float* dst = p.c.weights + static_cast<size_t>(head) * p.c.cap + token;
+      *dst = (p.decay == 0.f ? 0.f : p.decay * *dst) + (q ? sum[1] : sum[0]);
+    }
+  }
+}
+
 }  // namespace hc

@@ -181,6 +181,7 @@ def test_which_kernels_a_call_launches():
     assert c.attend(PTR, PTR, None, 4, at, 60 << 20, None) == 0 and launches() == ["packed_rows_kernel", "packed_merge_rows_kernel"]
     assert c.attend(PTR, PTR, None, 5, at, 60 << 20, None) == 0 and launches() == ["packed_attn_kernel", "packed_merge_kernel"]
     assert c.observe(PTR, PTR, 5, 1.0, at, 60 << 20, None) == 0 and launches() == ["packed_observe_kernel", "packed_observe_merge_kernel"]
+    assert c.observe(PTR, PTR, 4, 1.0, at, 60 << 20, None) == 0 and launches() == ["packed_observe_rows_kernel"]
     assert c.observe(PTR, PTR, 0, 0.5, None, 0, None) == 0 and launches() == ["packed_decay_kernel"]
     assert c.observe(PTR, PTR, 0, 1.0, None, 0, None) == 0 and launches() == []
 
