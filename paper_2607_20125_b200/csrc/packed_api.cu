@@ -114,8 +114,9 @@ T step_line(const headcast_packed* c, T (&first)[PACK_MAX_HEADS + 1], T per_tile
   return total;
 }
 
-// Up to 16 rows per key/value head go to packed_rows_kernel: 16 x 32760 tokens, 12 heads of 128, 28 us; packed_attn_kernel, for which
-// 17 rows are as much work as 128, takes 48.
+// Up to 16 rows per key/value head go to packed_rows_kernel: 16 x 32760 tokens, 12 heads of 128, 27 us; packed_attn_kernel, for which
+// 17 rows are as much work as 128, takes 48.  Observing, packed_observe_rows_kernel takes 11.8 us for 16 rows (9.1 for one), and
+// packed_observe_kernel 32 for 17.
 bool few_rows(const headcast_packed* c, int32_t n_queries) { return static_cast<int64_t>(n_queries) * (c->cfg.n_heads / c->cfg.n_kv_heads) <= ROWS_MAX; }
 
 struct RowsWorkspace {
@@ -147,7 +148,7 @@ int attend_few(headcast_packed* c, const void* q, void* out, float* lse, int32_t
   const int total = step_line(c, p.tile_first, 1);
   p.n_cta = std::min(c->n_sm, total);
   if (total > 0) {
-    const bool one = p.n_rows <= 8;  // 32760 tokens, 12 heads of 128: 21.4 us; with two tiles of queries 28.3
+    const bool one = p.n_rows <= 8;  // 32760 tokens, 12 heads of 128: 18.1 us; with two tiles of queries 26.7
     const int smem = RowsSmem<D>::DYN_BYTES;
     auto* kernel = one ? packed_rows_kernel<D, 1> : packed_rows_kernel<D, 2>;
     const int rc = allow_smem(c, one ? KERNEL_ROWS : KERNEL_ROWS_16, kernel, smem);

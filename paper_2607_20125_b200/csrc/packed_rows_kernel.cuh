@@ -3,18 +3,19 @@
 // The work is reading the cache, 9/16 byte per element, and turning four-bit codes into tensor-core operands.  The tiles of 128
 // tokens of all heads are laid end to end and every CTA (one per SM) takes an equal share; whatever part of a head it meets becomes
 // a partial result (running maximum, sum, unnormalised output), and packed_merge_rows_kernel joins the parts of each row.
-//   - bulk copies feed a ring of tiles (codes and scales are contiguous per head), groups of eight warps take the tiles in
-//     turn, each warp 16 of a tile's tokens with a running maximum and outputs of its own;
+//   - two groups of eight warps take the tiles in turn, each warp 16 of a tile's tokens with a running maximum and outputs of its
+//     own.  Codes and scales go straight into the registers that their conversion reads, which are filled for the next tile as soon as
+//     they have been used; with a ring of bulk copies in shared memory, whatever its depth, one query took 21.3 us instead of 18.1 over 32760 tokens and 59
+//     instead of 52 over 131072, 16 queries 28.0 instead of 26.7 and 76 instead of 83;
 //   - S^T = K Q^T and O^T += V^T P^T are m16n8k16 products, tokens (then value elements) on the 16 rows and eight queries on
 //     the columns: with the queries on the 16 rows there were twice the products.  A product's inner index may be permuted at will, so a
 //     lane multiplies the quarter of a row that it read with one load, and for V it reads the same 16 elements of two
 //     tokens and interleaves their codes before conversion; P is turned around by movmatrix;
 //   - the maximum is only looked for, across lanes, when some logit outgrows the reference;
-//   - the last of a stage's warps to leave it starts the next load into it: the ring is never short of copies in flight;
 //   - operands are fp16: held values are exact in it, query rows are brought to a common power of two first (see row_factor), and
 //     probabilities keep 11 bits.  tcgen05 products want 128 rows, eight times the conversions' share here.
-// One query, 12 heads of 128: 21.4 us for 32760 tokens (2.6 TB/s), 59.6 for 131072 (3.8 TB/s); without its arithmetic 11.8 and 38.9, without
-// its loads 18.9 and 49.2: the conversions bound it, the integer pipe is half busy.  8 us of a call are launches, first loads and the merge.
+// One query, 12 heads of 128: 18.1 us for 32760 tokens (3.1 TB/s), 52 for 131072 (4.3 TB/s).  Turning codes into operands bounds it, the
+// integer pipe is the busiest; 8 us of the first are launches, first loads and the merge.
 #pragma once
 #include "packed_format.cuh"
 
@@ -37,6 +38,7 @@ struct PackedRowsParams {
   int32_t tile_first[PACK_MAX_HEADS + 1];
   HeadCounts len;
 };
+
 // 8 x 8 values of 16 bits, two of a row per lane: the same with rows and columns exchanged.
 __device__ __forceinline__ uint32_t turn_8x8(uint32_t v) {
   uint32_t d;
@@ -46,13 +48,8 @@ __device__ __forceinline__ uint32_t turn_8x8(uint32_t v) {
 
 template <int D>
 struct RowsSmem {
-  static constexpr int CODES = PACK_TILE * D / 2, SCALES = PACK_TILE * D / PACK_GROUP;
-  static constexpr int STAGE = 2 * (CODES + SCALES);  // K codes, V codes, K scales, V scales
-  static constexpr int STAGES = D == 128 ? 6 : 12;    // a multiple of the groups: a stage belongs to one of them
-  static constexpr int Q_OFF = STAGES * STAGE;        // [D / 16][2 query tiles][32 lanes] uint2
-  static constexpr int MERGE_OFF = Q_OFF + D / 16 * 512;
-  static constexpr int MERGE = ROWS_GROUPS * ROWS_GROUP_WARPS * 8 * D * 4;
-  static constexpr int DYN_BYTES = MERGE_OFF + MERGE + 128;
+  static constexpr int Q_BYTES = D / 16 * 512;  // [D / 16][2 query tiles][32 lanes] uint2
+  static constexpr int DYN_BYTES = Q_BYTES + ROWS_GROUPS * ROWS_GROUP_WARPS * 8 * D * 4;  // and every warp's outputs
 };
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -94,16 +91,11 @@ __device__ __forceinline__ void stage_row(uint2* qs, float* row_scale, const __n
 // NQ: tiles of eight query rows
 template <int D, int NQ>
 __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __grid_constant__ PackedRowsParams p) {
-  using SM = RowsSmem<D>;
   constexpr int GROUPS = ROWS_GROUPS, WARPS = GROUPS * ROWS_GROUP_WARPS;
   constexpr int KW = D / 32;  // words of a key row that a lane reads
   constexpr int W = D / 8;    // elements of a value row that a lane reads
   constexpr int NT = D / 16;  // row tiles of O^T
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = aligned_shared<128>(smem_raw);
-  __shared__ uint64_t bar_full[SM::STAGES];
-  __shared__ int done[SM::STAGES], loads[SM::STAGES];  // warps that have left a stage's tile; copies into the stage so far
-  __shared__ int abort_flag;
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float row_scale[ROWS_MAX];
   __shared__ float warp_m[WARPS][ROWS_MAX], warp_l[WARPS][ROWS_MAX];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -111,46 +103,60 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
   const int t_lo = static_cast<int>(share_begin(blockIdx.x, total, p.n_cta)), t_hi = static_cast<int>(share_begin(blockIdx.x + 1, total, p.n_cta));
   int head = 0;
   while (p.tile_first[head + 1] <= t_lo) ++head;
-  // Loads tile t_lo + i into its stage.  The warp that is the last to leave a stage does it, at once.  (A warp of its own for the loads would
-  // cost a quarter of the registers: blocks get them for four warps at a time.)
-  auto load_tile = [&](int i, int from_head) {
-    const int t = t_lo + i, st = i % SM::STAGES;
-    while (p.tile_first[from_head + 1] <= t) ++from_head;
-    const size_t row = static_cast<size_t>(from_head) * p.c.cap + static_cast<size_t>(t - p.tile_first[from_head]) * PACK_TILE;
-    uint8_t* dst = smem + st * SM::STAGE;
-    ++loads[st];
-    mbar_arrive_expect_tx(&bar_full[st], SM::STAGE);
-    bulk_load(dst, p.c.k_codes + row * (D / 2), SM::CODES, &bar_full[st]);
-    bulk_load(dst + 2 * SM::CODES, p.c.k_scales + row * (D / PACK_GROUP), SM::SCALES, &bar_full[st]);
-    bulk_load(dst + SM::CODES, p.c.v_codes + row * (D / 2), SM::CODES, &bar_full[st]);
-    bulk_load(dst + 2 * SM::CODES + SM::SCALES, p.c.v_scales + row * (D / PACK_GROUP), SM::SCALES, &bar_full[st]);
-  };
-  if (tid == 0) {
-    for (int s = 0; s < SM::STAGES; ++s) {
-      mbar_init(&bar_full[s], 1);
-      done[s] = loads[s] = 0;
-    }
-    abort_flag = 0;
-    fence_mbar_init();
-  }
-  pdl_launch_dependents();
-  pdl_wait();
-  if (tid == 0)
-    for (int i = 0; i < min(t_hi - t_lo, SM::STAGES); ++i) load_tile(i, head);
-  volatile int* abortp = &abort_flag;
   const int group = warp / ROWS_GROUP_WARPS, key0 = (warp % ROWS_GROUP_WARPS) * 16;
   const int r = lane >> 2, q = lane & 3;
-  uint2* qs = reinterpret_cast<uint2*>(smem + SM::Q_OFF);
-  float* merge = reinterpret_cast<float*>(smem + SM::MERGE_OFF);
-  // Row c of a product's eight tokens is token c ^ ((c >> 1) & 1): neighbouring rows differ in their parity (K: two rows of 64
-  // bytes per 128-byte phase), and so do every other two (V).
-  const int key_row = r ^ ((r >> 1) & 1);
-  const int val_a = (2 * q) ^ (q & 1), val_b = (2 * q + 1) ^ (q & 1);
-  bool ok = true;  // cleared by an expired wait; the barriers of the block are met all the same
-  int mine = group, st = group, parity = 0;  // this group's next tile, counted from t_lo, and its stage
+  uint2* qs = reinterpret_cast<uint2*>(smem);
+  float* merge = reinterpret_cast<float*>(smem + RowsSmem<D>::Q_BYTES);
+  // What a lane reads of a tile: a quarter of the keys of two tokens, 16 elements of the values of four; the rows of S^T are the
+  // tokens key0 + r and key0 + 8 + r, and P^T wants those of rows 2q and 2q + 1 of both halves.
+  uint32_t kw[2][KW], k_scales[2];
+  constexpr int VW = W / 8;  // words
+  uint32_t va[2][VW], vb[2][VW], v_scales[2][2];
+  auto fetch_k = [&](int h, int tile) {
+    const size_t row0 = static_cast<size_t>(h) * p.c.cap + static_cast<size_t>(tile) * PACK_TILE + key0 + r;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const size_t row = row0 + 8 * j;
+      if (D == 128) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p.c.k_codes + row * (D / 2) + q * 16);
+        kw[j][0] = v.x; kw[j][1] = v.y; kw[j][KW - 2] = v.z; kw[j][KW - 1] = v.w;
+        k_scales[j] = *reinterpret_cast<const uint16_t*>(p.c.k_scales + row * (D / PACK_GROUP) + q * 2);
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(p.c.k_codes + row * (D / 2) + q * 8);
+        kw[j][0] = v.x; kw[j][1] = v.y;
+        k_scales[j] = p.c.k_scales[row * (D / PACK_GROUP) + q];
+      }
+    }
+  };
+  auto fetch_v = [&](int h, int tile) {
+    const size_t row0 = static_cast<size_t>(h) * p.c.cap + static_cast<size_t>(tile) * PACK_TILE + key0 + 2 * q;
+    const int g = r * W / PACK_GROUP;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const size_t row = row0 + 8 * j;
+      if (D == 128) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p.c.v_codes + row * (D / 2) + r * 8), y = *reinterpret_cast<const uint2*>(p.c.v_codes + (row + 1) * (D / 2) + r * 8);
+        va[j][0] = x.x; va[j][VW - 1] = x.y;
+        vb[j][0] = y.x; vb[j][VW - 1] = y.y;
+      } else {
+        va[j][0] = *reinterpret_cast<const uint32_t*>(p.c.v_codes + row * (D / 2) + r * 4);
+        vb[j][0] = *reinterpret_cast<const uint32_t*>(p.c.v_codes + (row + 1) * (D / 2) + r * 4);
+      }
+      v_scales[j][0] = p.c.v_scales[row * (D / PACK_GROUP) + g];
+      v_scales[j][1] = p.c.v_scales[(row + 1) * (D / PACK_GROUP) + g];
+    }
+  };
+  pdl_launch_dependents();
+  pdl_wait();
+  int mine = group;  // this group's next tile, counted from t_lo
   for (int t0 = t_lo; t0 < t_hi; ++head) {
     const int t1 = min(t_hi, p.tile_first[head + 1]);
     if (t1 <= t0) continue;  // a head without tokens
+    const int first = t_lo - p.tile_first[head];  // of this head's tiles, where `mine` is 0
+    if (mine < t1 - t_lo) {
+      fetch_k(head, first + mine);
+      fetch_v(head, first + mine);
+    }
     if (warp < 8 * NQ) {
       const int token = warp / p.group, h = head * p.group + warp % p.group;
       stage_row<D>(qs, row_scale, p.q + (static_cast<size_t>(token) * (p.c.n_kv * p.group) + h) * D, warp, warp < p.n_rows, p.scale_log2e);
@@ -172,40 +178,20 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
     const int last_tile = p.tile_first[head + 1] - 1 - t_lo;  // of the head
     const int last_valid = p.len.n[head] - (last_tile + t_lo - p.tile_first[head]) * PACK_TILE - key0;  // of this warp's 16 tokens there
     for (; mine < t1 - t_lo; mine += GROUPS) {
-      if (ok) ok = mbar_wait_warp(&bar_full[st], parity, abortp, p.c.status, 63);
-      if (!ok) break;
-      const uint8_t* kc = smem + st * SM::STAGE;
-      const uint8_t* vc = kc + SM::CODES;
-      const uint8_t* ks = kc + 2 * SM::CODES;
-      const uint8_t* vs = ks + SM::SCALES;
       // S^T: 16 tokens
-      float s[NQ][4], s_odd[NQ][4];  // two chains of products
+      float s[NQ][4], s_odd[NQ][4];  // two chains of products (one where registers are short)
 #pragma unroll
       for (int z = 0; z < NQ; ++z)
 #pragma unroll
         for (int y = 0; y < 4; ++y) s[z][y] = s_odd[z][y] = 0.f;
       {
-        uint32_t w[2][KW], scales[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int row = key0 + 8 * j + key_row;
-          if (D == 128) {
-            const uint4 v = *reinterpret_cast<const uint4*>(kc + row * (D / 2) + q * 16);
-            w[j][0] = v.x; w[j][1] = v.y; w[j][KW - 2] = v.z; w[j][KW - 1] = v.w;
-            scales[j] = *reinterpret_cast<const uint16_t*>(ks + row * (D / PACK_GROUP) + q * 2);
-          } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(kc + row * (D / 2) + q * 8);
-            w[j][0] = v.x; w[j][1] = v.y;
-            scales[j] = *(ks + row * (D / PACK_GROUP) + q);
-          }
-        }
 #pragma unroll
         for (int x = 0; x < KW; ++x) {
           uint32_t a[2][4];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t sc = scale_f16x2(scales[j], x / 2);
-            codes_to_f16x2(w[j][x], a[j]);
+            const uint32_t sc = scale_f16x2(k_scales[j], x / 2);
+            codes_to_f16x2(kw[j][x], a[j]);
 #pragma unroll
             for (int y = 0; y < 4; ++y) a[j][y] = mul_f16x2(a[j][y], sc);
           }
@@ -213,19 +199,22 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
           for (int z = 0; z < NQ; ++z) {
             const uint2 b0 = qs[(4 * x + z) * 32 + lane], b1 = qs[(4 * x + 2 + z) * 32 + lane];
             mma_16816(s[z], a[0][0], a[1][0], a[0][1], a[1][1], b0.x, b0.y);
-            mma_16816(s_odd[z], a[0][2], a[1][2], a[0][3], a[1][3], b1.x, b1.y);
+            mma_16816(NQ == 1 ? s_odd[z] : s[z], a[0][2], a[1][2], a[0][3], a[1][3], b1.x, b1.y);
           }
         }
 #pragma unroll
         for (int z = 0; z < NQ; ++z)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) s[z][y] += s_odd[z][y];
+          for (int y = 0; y < 4; ++y) s[z][y] += NQ == 1 ? s_odd[z][y] : 0.f;
       }
+      // the registers are filled for the group's next tile as soon as they have been used
+      const bool more = mine + GROUPS < t1 - t_lo;
+      if (more) fetch_k(head, first + mine + GROUPS);
       if (mine == last_tile) {
 #pragma unroll
         for (int z = 0; z < NQ; ++z) {
-          if (key_row >= last_valid) s[z][0] = s[z][1] = -INFINITY;
-          if (8 + key_row >= last_valid) s[z][2] = s[z][3] = -INFINITY;
+          if (r >= last_valid) s[z][0] = s[z][1] = -INFINITY;
+          if (8 + r >= last_valid) s[z][2] = s[z][3] = -INFINITY;
         }
       }
       // The reference moves only when some logit outgrows it (a NaN never does); tokens that are not there leave it.
@@ -273,30 +262,17 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
       }
       // O^T += V^T P^T: this lane's W elements of the tokens of rows 2q and 2q + 1 of both halves
       {
-        constexpr int VW = W / 8;  // words
-        uint32_t a[2][VW], b[2][VW], sc[2];
+        uint32_t sc[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int ra = key0 + 8 * j + val_a, rb = key0 + 8 * j + val_b;
-          if (D == 128) {
-            const uint2 x = *reinterpret_cast<const uint2*>(vc + ra * (D / 2) + r * 8), y = *reinterpret_cast<const uint2*>(vc + rb * (D / 2) + r * 8);
-            a[j][0] = x.x; a[j][VW - 1] = x.y;
-            b[j][0] = y.x; b[j][VW - 1] = y.y;
-          } else {
-            a[j][0] = *reinterpret_cast<const uint32_t*>(vc + ra * (D / 2) + r * 4);
-            b[j][0] = *reinterpret_cast<const uint32_t*>(vc + rb * (D / 2) + r * 4);
-          }
-          const int g = r * W / PACK_GROUP;
-          sc[j] = pack_f16x2(scale_value(vs[ra * (D / PACK_GROUP) + g], 0), scale_value(vs[rb * (D / PACK_GROUP) + g], 0));
-        }
+        for (int j = 0; j < 2; ++j) sc[j] = pack_f16x2(scale_value(v_scales[j][0], 0), scale_value(v_scales[j][1], 0));
 #pragma unroll
         for (int x = 0; x < VW; ++x) {
           uint32_t even[2][4], odd[2][4];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             constexpr uint32_t LOW = 0x0f0f0f0fu;
-            codes_to_f16x2((a[j][x] & LOW) | ((b[j][x] << 4) & ~LOW), even[j]);
-            codes_to_f16x2(((a[j][x] >> 4) & LOW) | (b[j][x] & ~LOW), odd[j]);
+            codes_to_f16x2((va[j][x] & LOW) | ((vb[j][x] << 4) & ~LOW), even[j]);
+            codes_to_f16x2(((va[j][x] >> 4) & LOW) | (vb[j][x] & ~LOW), odd[j]);
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
               even[j][y] = mul_f16x2(even[j][y], sc[j]);
@@ -309,20 +285,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
             for (int z = 0; z < NQ; ++z) mma_16816(o[z][4 * x + y], even[0][y], odd[0][y], even[1][y], odd[1][y], pt[z][0], pt[z][1]);
         }
       }
-      __syncwarp();
-      if (lane == 0) {
-        __threadfence_block();
-        if (atomicAdd(&done[st], 1) == ROWS_GROUP_WARPS - 1) {
-          done[st] = 0;
-          if (mine + SM::STAGES < t_hi - t_lo) load_tile(mine + SM::STAGES, head);
-        }
-      }
-      __syncwarp();
-      st += GROUPS;
-      if (st >= SM::STAGES) {
-        st -= SM::STAGES;
-        parity ^= 1;
-      }
+      if (more) fetch_v(head, first + mine + GROUPS);
     }
     // ---- the warps' results become one, relative to the largest reference, through shared memory
 #pragma unroll
@@ -338,7 +301,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
       }
     __syncthreads();
     const int slot = blockIdx.x + head;
-    if (ok && tid < p.n_rows) {
+    if (tid < p.n_rows) {
       float top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int x = 0; x < WARPS; ++x) top = fmaxf(top, warp_m[x][tid]);
@@ -364,7 +327,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
       }
       __syncthreads();
       const int query = tid / (D / 4), chunk = tid % (D / 4);
-      if (query < 8 && 8 * z + query < p.n_rows && ok) {
+      if (query < 8 && 8 * z + query < p.n_rows) {
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int x = 0; x < WARPS; ++x) {
@@ -376,12 +339,6 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
       __syncthreads();  // what was read here is overwritten by the next tile of queries, or the next head's rows
     }
     t0 = t1;
-  }
-  if (*abortp != 0 && tid == 0) {  // the copies in flight land before the block leaves
-    for (int x = 0; x < SM::STAGES; ++x) {
-      int local_abort = 0;
-      if (loads[x] > 0) mbar_wait(&bar_full[x], (loads[x] - 1) & 1, &local_abort, p.c.status, 62);
-    }
   }
 }
 
@@ -399,7 +356,6 @@ __global__ void __launch_bounds__(MERGE_GROUPS * D / 4) packed_merge_rows_kernel
   const int total = p.tile_first[p.c.n_kv], first = p.tile_first[head], last = p.tile_first[head + 1] - 1;
   const int b0 = last >= first ? share_owner(first, total, p.n_cta) : 0, n = last >= first ? share_owner(last, total, p.n_cta) - b0 + 1 : 0;
   pdl_wait();
-  if (*reinterpret_cast<volatile int32_t*>(p.c.status) != 0) return;  // a part is missing
   float m = -INFINITY, l = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = g; i < n; i += MERGE_GROUPS) {
@@ -437,8 +393,8 @@ __global__ void __launch_bounds__(MERGE_GROUPS * D / 4) packed_merge_rows_kernel
 // What up to 16 query rows per key/value head give to every token: weight = decay * weight + sum over the rows of exp(logit - lse).
 // The products are those of packed_rows_kernel without the values; a row of S^T is a token and its columns the queries, so a
 // token's sum is four lanes' to add and each token belongs to one warp: no parts, no second kernel.  Keys are read straight into registers, a
-// tile ahead; 73 bytes per token and head at d = 128.  One query, 32760 tokens, 12 heads of 128: OBS_ROWS_US us (packed_observe_kernel, for
-// which one query is as much work as 32: 32).
+// tile ahead; 80 bytes per token and head at d = 128.  One query, 32760 tokens, 12 heads of 128: 9.1 us (3.4 TB/s;
+// packed_observe_kernel, for which one query is as much work as 32: 32); 131072 tokens 29.5 (4.3).  Conversions bound it.
 struct PackedObserveRowsParams {
   PackedView c;
   const __nv_bfloat16* q;
