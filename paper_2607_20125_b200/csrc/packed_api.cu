@@ -281,6 +281,7 @@ int headcast_rope(const headcast_rope_config* cfg, const void* q, void* q_out, i
     for (int j = 0; j < (k ? 2 : 1); ++j) {
       const bool same = i == j && src[i] == dst[i] && p.src_stride[i] == heads[i] * d;
       if (!same && overlap(src[i], src_bytes[i], dst[j], dst_bytes[j])) return rope_fail(HC_ERR_INVALID_ARG, "an output overlaps an input that it is not");
+      if (i == j && positions && overlap(positions, 12ll * n_tokens, dst[i], dst_bytes[i])) return rope_fail(HC_ERR_INVALID_ARG, "an output overlaps the positions");
       if (i < j && overlap(dst[i], dst_bytes[i], dst[j], dst_bytes[j])) return rope_fail(HC_ERR_INVALID_ARG, "the outputs overlap");
     }
   p.n = n_tokens;
@@ -463,6 +464,8 @@ int headcast_packed_attend(headcast_packed* c, const void* q, void* out, float* 
   const int64_t q_bytes = 2ll * n_queries * c->cfg.n_heads * c->cfg.head_dim;
   if (q != out && overlap(q, q_bytes, out, q_bytes)) return fail(c, HC_ERR_INVALID_ARG, "out overlaps q without being q");
   if (lse && !aligned(lse, 4)) return fail(c, HC_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  const int64_t lse_bytes = 4ll * n_queries * c->cfg.n_heads;
+  if (lse && (overlap(lse, lse_bytes, q, q_bytes) || overlap(lse, lse_bytes, out, q_bytes))) return fail(c, HC_ERR_INVALID_ARG, "lse overlaps q or out");
   if (!aligned(workspace, 256) || workspace_bytes < headcast_packed_workspace_bytes(c, n_queries))
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_workspace_bytes(%d)", n_queries);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

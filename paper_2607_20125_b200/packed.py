@@ -281,7 +281,7 @@ class PackedCache:
             raise ValueError("other: expected a PackedCache")
         ptr, width, ws, size = None, 0, None, 0
         if index is not None:
-            width = index.shape[1] if isinstance(index, torch.Tensor) and index.dim() == 2 else -1
+            width = _int(index.shape[1], "index") if isinstance(index, torch.Tensor) and index.dim() == 2 else -1
             ptr = _tensor(index, "index", (kv, width), torch.int32, device)
         else:
             size = lib.headcast_packed_evict_workspace_bytes(self._ptr)

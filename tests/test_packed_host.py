@@ -239,3 +239,16 @@ def test_rotation_refusals():
     rc, error = rope(halves=1, dim_t=20)
     assert rc == UNSUPPORTED and "16" in error
     assert rope(n=0, q=None, q_out=None)[0] == 0
+
+
+def test_outputs_that_overlap_smaller_inputs_and_outputs():
+    c = Cache()
+    assert c.append(PTR, PTR, 50, 0, None) == 0
+    launches()
+    ws, q_bytes = c.workspace_bytes(8), 8 * 4 * 64 * 2
+    for lse in (PTR, PTR + q_bytes - 4, PTR + 65536 - 4, PTR + 65536 + q_bytes - 4):
+        assert c.attend(PTR, PTR + 65536, C.c_void_p(lse), 8, PTR + 131072, ws, None) == INVALID and "lse overlaps" in c.error()
+    assert launches() == []
+    assert c.attend(PTR, PTR + 65536, C.c_void_p(PTR + q_bytes), 8, PTR + 131072, ws, None) == 0
+    rc, error = rope(pos=PTR + 65536 + 4)
+    assert rc == INVALID and "positions" in error
