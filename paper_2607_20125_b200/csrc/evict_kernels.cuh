@@ -1,7 +1,7 @@
 // Eviction from a packed cache: which tokens of a head stay, and their move into another cache.
 //
-// evict_select_kernel, one cluster of up to 8 blocks per head: the keep-th largest weight by radix selection (three digits of
-// 11, 11 and 10 bits of an order-preserving integer), then the places of all tokens above it, and of the first ones equal to it, in
+// evict_select_kernel, one cluster of up to 8 blocks per head: the keep-th largest weight by radix selection (up to three digits
+// of 11, 11 and 10 bits of an order-preserving integer), then the places of all tokens above it, and of the first ones equal to it, in
 // order.  The blocks of a cluster split the head's tokens, a warp a run of them; each block finds the digit for itself from the
 // histograms of all, first among 64 sums of 32 bins, then among that group's bins, so that little crosses between the blocks (all
 // 2048 bins read from all blocks took 2.7 us a digit).  Counts are integers and places follow from prefix sums, so the result is
@@ -54,8 +54,9 @@ __device__ __forceinline__ uint32_t peer_word(const uint32_t* p, uint32_t rank) 
 }
 constexpr int SELECT_MAX_BLOCKS = 8;  // of a cluster
 
-// Of n counts (64 or 32, one per thread of the first warps), highest first: which one holds the k-th key, and the rank in it.  The whole
-// block calls it; the counts lie in `sums`, the answer goes to `found`.
+// Of n counts (64 or 32, two or one per lane of the first warp), highest first: which one holds the k-th key, the rank in it, and the
+// count.  The whole block calls it; the counts lie in `sums`, the answer goes to `found`.  Its barriers also keep the counts of one call
+// from the reads of the one before, and the answers likewise.
 template <int N>
 __device__ __forceinline__ void find_kth(const uint32_t* sums, uint32_t k, uint32_t* found) {
   const int tid = threadIdx.x;
@@ -77,6 +78,7 @@ __device__ __forceinline__ void find_kth(const uint32_t* sums, uint32_t k, uint3
       if (above < k && k <= above + c[i]) {  // exactly one lane, once
         found[0] = tid * PER + i;
         found[1] = k - above;
+        found[2] = c[i];
       }
       above += c[i];
     }
@@ -84,14 +86,19 @@ __device__ __forceinline__ void find_kth(const uint32_t* sums, uint32_t k, uint3
   __syncthreads();
 }
 
+// ONE: clusters of one block, whose barriers and reads are the block's own (3003 tokens of 6 heads, selection and move: 9.7 us, as a cluster 11.7).
+template <bool ONE>
 __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __grid_constant__ SelectParams p) {
   __shared__ uint32_t hist[2][SELECT_BINS], groups[2][SELECT_GROUPS];  // used in turn: one cluster barrier per digit
-  __shared__ uint32_t sums[SELECT_GROUPS], found[2], counts[2], warp_gt[32], warp_eq[32];
+  __shared__ uint32_t sums[SELECT_GROUPS], found[3], counts[2], warp_gt[32], warp_eq[32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t rank = cluster_rank(), ranks = cluster_size();
+  const uint32_t rank = ONE ? 0u : cluster_rank(), ranks = ONE ? 1u : cluster_size();
+  auto sync_all = [] { ONE ? __syncthreads() : cluster_sync(); };
+  auto word_of = [](const uint32_t* p, uint32_t rank) { return ONE ? *p : peer_word(p, rank); };
   const int h = blockIdx.x / ranks;
   const int n = p.len.n[h], keep = p.keep.n[h];
   pdl_launch_dependents();
+  for (int b = tid; b < 2 * SELECT_BINS; b += SELECT_THREADS) (&hist[0][0])[b] = 0;
   pdl_wait();
   if (keep <= 0) return;  // the same for the whole cluster
   const int lo = static_cast<int>(static_cast<long long>(n) * rank / ranks), hi = static_cast<int>(static_cast<long long>(n) * (rank + 1) / ranks);
@@ -127,13 +134,12 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
     }
   };
 
+  __syncthreads();
   uint32_t prefix = 0, mask = 0, k = keep;  // the k-th largest of the keys that agree with prefix under mask
 #pragma unroll 1
   for (int digit = 0; digit < 3; ++digit) {
     const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
     uint32_t* mine = hist[digit & 1];
-    for (int b = tid; b < SELECT_BINS; b += SELECT_THREADS) mine[b] = 0;
-    __syncthreads();
     each([&](int, uint32_t key, bool there) {
       const bool counts_in = there && (key & mask) == prefix;
       // Equal weights are common (tokens that nothing has looked at yet), and a warp of them would add to one bin 32 times in turn:
@@ -154,10 +160,12 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
       const uint32_t sum = __reduce_add_sync(0xffffffffu, mine[(2 * warp + x) * 32 + lane]);
       if (lane == 0) groups[digit & 1][2 * warp + x] = sum;
     }
-    cluster_sync();
+    sync_all();
+    if (digit == 1)  // the first digit's bins are the third's; all blocks have read them
+      for (int b = tid; b < SELECT_BINS; b += SELECT_THREADS) hist[0][b] = 0;
     // eight lanes per group, and then per bin: one for each block
     if (tid < 8 * SELECT_GROUPS) {
-      uint32_t c = (tid & 7) < ranks ? peer_word(&groups[digit & 1][tid >> 3], tid & 7) : 0u;
+      uint32_t c = (tid & 7) < ranks ? word_of(&groups[digit & 1][tid >> 3], tid & 7) : 0u;
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
       if ((tid & 7) == 0) sums[tid >> 3] = c;
@@ -165,9 +173,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
     find_kth<SELECT_GROUPS>(sums, k, found);
     const uint32_t group = found[0];
     k = found[1];
-    __syncthreads();
     if (tid < 8 * 32) {
-      uint32_t c = (tid & 7) < ranks ? peer_word(&mine[group * 32 + (tid >> 3)], tid & 7) : 0u;
+      uint32_t c = (tid & 7) < ranks ? word_of(&mine[group * 32 + (tid >> 3)], tid & 7) : 0u;
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
       if ((tid & 7) == 0) sums[tid >> 3] = c;
@@ -176,9 +183,9 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
     prefix |= (group * 32 + found[0]) << shift;
     mask |= ((1u << bits) - 1u) << shift;
     k = found[1];
-    __syncthreads();
+    if (k == found[2]) break;  // all of that bin stay (in most cases it holds one key by the second digit)
   }
-  // `prefix` is the keep-th largest key, and k tokens of that key stay: the first ones
+  // `prefix` is the keep-th largest key, and k tokens of that key stay: the first ones.  (Or all keys from `prefix` on stay.)
   uint32_t n_gt = 0, n_eq = 0;
   each([&](int, uint32_t key, bool there) {
     n_gt += __popc(__ballot_sync(0xffffffffu, there && key > prefix));
@@ -196,12 +203,12 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
       counts[1] = e;
     }
   }
-  cluster_sync();
+  sync_all();
   // of the tokens before this warp's: those of the blocks before, then of the warps before
   uint32_t gt = 0, eq = 0;
   if (lane < rank) {
-    gt = peer_word(&counts[0], lane);
-    eq = peer_word(&counts[1], lane);
+    gt = word_of(&counts[0], lane);
+    eq = word_of(&counts[1], lane);
   }
   if (lane < warp) {
     gt += warp_gt[lane];
@@ -219,7 +226,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
     gt += __popc(m_gt);
     eq += __popc(m_eq);
   });
-  cluster_sync();  // no block leaves while another may read its shared memory
+  if (!ONE) cluster_sync();  // no block leaves while another may read its shared memory
 }
 
 struct EvictMoveParams {

@@ -578,8 +578,8 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     s.cap = c->view.cap;
     s.n_first = n_first;
     s.n_recent = n_recent;
-    // Blocks per head, 4096 tokens each: 1000 tokens 10.8 us with one block and 12.4 with eight, 9000 17.8 / 15.0 (four), 75600 189 / 46.8
-    // (eight; selection and move, 12 heads of 128).
+    // Blocks per head, 4096 tokens each: selection and move of 9000 tokens, 12 heads of 128, 14.7 us with four and 17.2 with one, 12000
+    // 15.7 / 20.3, 5000 11.7-13.1 with two or one; with eight blocks 1000 tokens took 1.6 us more than with a cluster of one.
     int blocks = 1;
     while (blocks < SELECT_MAX_BLOCKS && blocks * 4096 < longest) blocks *= 2;
     cudaLaunchConfig_t lc = {};
@@ -594,7 +594,7 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
     lc.numAttrs = 2;
-    PK_CUDA(c, cudaLaunchKernelEx(&lc, evict_select_kernel, s));
+    PK_CUDA(c, cudaLaunchKernelEx(&lc, blocks == 1 ? evict_select_kernel<true> : evict_select_kernel<false>, s));
     EvictMoveParams m;
     std::memset(&m, 0, sizeof(m));
     m.src = c->view;

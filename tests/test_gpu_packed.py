@@ -513,6 +513,26 @@ def test_eviction_of_long_heads():
     check_evict(cache, [n // 3], 10, 1000)
 
 
+@pytest.mark.parametrize("n", [512, 3000, 4096, 9000, 50000])
+def test_eviction_where_the_first_digits_settle_it(n):
+    """Numbers to keep that end with a digit's bin, one before and one behind: eight powers of two (first digit), 1 + i 2^-13 (second),
+    1 + i 2^-23 (third)."""
+    import torch
+    g = gen(n)
+    cache = make(3, 3, 64, n, randn(g, n, 3, 64), randn(g, n, 3, 64))
+    order = torch.randperm(n, device="cuda", generator=g)
+    w = cache.weights
+    w[0] = torch.exp2((order % 8).float())
+    w[1] = 1.0 + (order % 2048).float() * 2.0 ** -13
+    w[2] = 1.0 + (order % 2048).float() * 2.0 ** -23
+    rows = [torch.sort(w[h], descending=True)[0] for h in range(3)]
+    for at in (1, n // 3, n // 2, n - 1):
+        ends = [int((rows[h] >= rows[h][at]).sum()) for h in range(3)]  # of the bin of the at-th largest
+        for off in (-1, 0, 1):
+            check_evict(cache, [min(n, max(0, e + off)) for e in ends], 0, 0)
+            check_evict(cache, [min(n, max(0, e + off)) for e in ends], 5, 20)
+
+
 def test_eviction_without_index_equals_that_with_one_and_is_captured():
     import torch
     g = gen(23)
