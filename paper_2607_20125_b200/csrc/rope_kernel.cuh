@@ -3,8 +3,9 @@
 // The angle is formed in turns, in 64-bit integers: a frequency is a fraction of a turn per position in units of 2^-64 turn, and
 // position * frequency modulo 2^64 is the exact fractional turn, for positions of any size and sign.  Its upper 32 bits go
 // to sincospif, so that a far position is as exact as a near one (an angle of 10^5 in fp32 is off by 4e-3).
-// Bound by memory: every value is read and written once, 4 bytes together; 24480 tokens of 12 + 12 heads of 128 in 54 us, 5.5 TB/s.  A block forms the sines and cosines of its tokens once,
-// in shared memory, for all heads of queries and keys.
+// Bound by memory: every value is read and written once, 4 bytes together; 24480 tokens of 12 + 12 heads of 128 in 53 us, 5.7 TB/s.
+// A block forms the sines and cosines of its tokens once, in shared memory, for all heads of queries and keys.  (Two or four loads under
+// way per thread, with fewer blocks: 55 to 65 us.)
 #pragma once
 #include "tc05.cuh"
 
@@ -32,7 +33,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 8) rope_kernel(const __grid_cons
   extern __shared__ float2 turn[];  // [tokens_per_block][D / 2] cosine and sine
   constexpr int PAIRS = D / 2;
   pdl_launch_dependents();
-  pdl_wait();
+  if (p.positions) pdl_wait();  // the grid's positions are this call's own: their sines are formed while the kernel before ends
   const int t0 = blockIdx.x * tokens_per_block, nt = min(tokens_per_block, p.n - t0);
   for (int i = threadIdx.x; i < nt * PAIRS; i += ROPE_THREADS) {
     const int token = t0 + i / PAIRS, pair = i % PAIRS;
@@ -52,6 +53,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 8) rope_kernel(const __grid_cons
     sincospif(half_turns, &s, &c);
     turn[i] = make_float2(c, s);
   }
+  if (!p.positions) pdl_wait();
   __syncthreads();
   // what a thread turns at a time: 16 bytes of a row, in halves the 16 bytes of the partners too
   constexpr int CHUNKS = D / 8;

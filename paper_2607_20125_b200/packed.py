@@ -176,6 +176,7 @@ class PackedCache:
             self._ptr = C.c_void_p()
             raise HeadCastError(rc, "headcast_packed_create failed")
         self._lengths = (C.c_int32 * self.n_kv_heads)()
+        self._like = self.storage[:0].view(torch.bfloat16)  # what exported tensors are made like
         stride = C.c_int64()
         at = self.lib.headcast_packed_weights_offset(self._ptr, C.byref(stride))
         self._weights = self.storage[at:at + 4 * stride.value * self.n_kv_heads].view(torch.float32).view(self.n_kv_heads, stride.value)
@@ -195,7 +196,7 @@ class PackedCache:
         raise HeadCastError(rc, self.lib.headcast_packed_last_error(self._ptr).decode())
 
     def _workspace(self, size: int):
-        return torch.empty(max(size, 0), dtype=torch.uint8, device=self._where)
+        return self.storage.new_empty(max(size, 0))
 
     @property
     def weights(self):
@@ -237,9 +238,12 @@ class PackedCache:
         n = max(0, max(lengths) - first) if n_tokens is None else _int(n_tokens, "n_tokens")
         if n < 0:
             raise ValueError(f"n_tokens must not be negative, got {n}")
-        make = torch.empty if first + n <= min(lengths) else torch.zeros
-        both = make((2, self.n_kv_heads, n, self.head_dim), dtype=torch.bfloat16, device=self._where)
-        k, v = both.unbind(0)
+        if first + n <= min(lengths):
+            k = self._like.new_empty((self.n_kv_heads, n, self.head_dim))
+            v = torch.empty_like(k)
+        else:
+            k = self._like.new_zeros((self.n_kv_heads, n, self.head_dim))
+            v = torch.zeros_like(k)
         rc = self.lib.headcast_packed_export(self._ptr, first, n, k.data_ptr() if n else None, v.data_ptr() if n else None, _raw_stream(self._device))
         if rc != 0:
             self._raise(rc)
