@@ -337,6 +337,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         mbar_arrive_if(&bar_q_full[t], lane == 0);
       }
       float m_ref = NO_REFERENCE, l_sum = 0.f;
+      bool seeking = true;  // some row of the warp has no reference yet
       for (int tile = w.tile_begin; tile < w.tile_end; ++tile) {
         const int n_valid = min(PACK_TILE, p.len.n[w.head] - tile * PACK_TILE);
         if (!(ok = mbar_wait_warp(&bar_s_full[t], s_cnt & 1, abortp, p.c.status, 78))) break;
@@ -348,11 +349,12 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
           tmem_wait_st();
         }
         // The exponentials are taken relative to the reference as it stands, without a look for the tile's maximum: their sum shows
-        // whether one of them outgrew fp16 (each is at most the sum).  Only then, and in an item's first tile, the maximum is
-        // found, the reference moved and the tile done again; the logits are still there, P is stored last.
+        // whether one of them outgrew fp16 (each is at most the sum).  Only then, and until every row of the warp has a reference of
+        // its own (mostly in an item's first tile), the maximum is found, the reference moved and the tile done again; the logits
+        // are still there, P is stored last.
         uint32_t pk[64];
         float tile_sum;
-        for (bool look = tile == w.tile_begin;; look = true) {
+        for (bool look = seeking;; look = true) {
           if (look) {
             float mx = -INFINITY;
 #pragma unroll 1
@@ -364,9 +366,9 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
               for (int i = 0; i < 32; i += 2) mx = max3(mx, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
             }
             mx *= c;
-            if (beyond_limit(mx)) c = __uint_as_float(0x7fffffffu);
+            if (above_limit(mx)) c = __uint_as_float(0x7fffffffu);
             if (__any_sync(0xffffffffu, mx > m_ref + P_HEADROOM + 1.f)) {
-              const float m_new = mx > m_ref + P_HEADROOM ? mx - P_HEADROOM : m_ref;
+              const float m_new = mx > m_ref + P_HEADROOM ? reference_for(mx) : m_ref;
               const float alpha = ex2_approx(m_ref - m_new);
               l_sum *= alpha;
               m_ref = m_new;
@@ -382,6 +384,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
                 }
               }
             }
+            seeking = __any_sync(0xffffffffu, m_ref <= LOWEST_REFERENCE);
           }
           const uint64_t c2 = pack_f32x2(c, c), m2 = pack_f32x2(-m_ref, -m_ref);
           uint64_t sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         l_sum += tile_sum;
       }
       if (!ok) break;
-      if (m_ref == NO_REFERENCE) m_ref = -INFINITY;  // nothing but NaNs
+      if (m_ref == NO_REFERENCE) m_ref = -INFINITY;  // no logit that is a number
       // ---- epilogue
       if (!(ok = mbar_wait_warp(&bar_o_full[t], o_cnt & 1, abortp, p.c.status, 79))) break;
       ++o_cnt;
@@ -431,6 +434,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
       // stores cover whole lines.
       uint8_t* stg = sq + row0 * 128;
       if (w.slot < 0) {
+        l_sum = final_sum(m_ref, l_sum);
         const float inv = 1.f / l_sum;  // positive, or NaN
 #pragma unroll 1
         for (int ch = 0; ch < D / 32; ++ch) {
@@ -578,6 +582,7 @@ __global__ void __launch_bounds__(16 * D / 8) packed_merge_kernel(const __grid_c
     m = top;
   }
   if (row >= p.n_rows) return;
+  l = final_sum(m, l);
   const float inv = 1.f / l;
   const int token = row / p.group, h = head * p.group + (row - token * p.group);
   uint4 o4;

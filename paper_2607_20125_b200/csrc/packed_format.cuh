@@ -127,9 +127,15 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 constexpr float P_HEADROOM = 6.f, P_LAG = 14.f;
 // The reference of a row that has met no logit yet (or only NaNs): below all of them, and finite, so that exponentials need no case for it.
 constexpr float NO_REFERENCE = -3e38f;
-// From here on (log2 domain) a reference in fp32 may be further from the largest logit than its exponential can stand: the row becomes NaN.
-constexpr float LOGIT_LIMIT = 4194304.f;
-__device__ __forceinline__ bool beyond_limit(float mx) { return fabsf(mx) >= LOGIT_LIMIT && mx != -INFINITY; }
+// From here on (log2 domain) a reference in fp32 may be further from the largest logit than its exponential can stand: a row whose largest
+// logit is not within -LOGIT_LIMIT .. LOGIT_LIMIT becomes NaN.  Upwards any logit shows it.  Downwards only all of the row's logits together
+// do: while none is above -LOGIT_LIMIT the reference stays at LOWEST_REFERENCE, below that of every other row, to which such tokens are
+// at most 2^P_LAG; one that stands there when all parts have been joined belongs to a row of NaNs.
+constexpr float LOGIT_LIMIT = 4194304.f, LOWEST_REFERENCE = -LOGIT_LIMIT - P_LAG;
+__device__ __forceinline__ bool above_limit(float mx) { return mx >= LOGIT_LIMIT; }
+__device__ __forceinline__ float reference_for(float mx) { return mx > -LOGIT_LIMIT ? mx - P_HEADROOM : LOWEST_REFERENCE; }
+// The sum of a row whose parts have all been joined, relative to reference m.
+__device__ __forceinline__ float final_sum(float m, float sum) { return m <= LOWEST_REFERENCE ? __uint_as_float(0x7fffffffu) : sum; }
 
 // The factor that brings a query row whose largest magnitude is `amax` to magnitudes below 2^15, and its inverse: powers of two, so
 // every element of a bf16 row that is not smaller than 2^-28 of the largest is exact in fp16, and the others are off by

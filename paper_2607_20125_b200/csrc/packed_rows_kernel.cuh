@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) packed_rows_kernel(const __gr
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
             mx *= c[z][y];
-            if (beyond_limit(mx)) c[z][y] = __uint_as_float(0x7fffffffu);
-            const float to = mx > m[z][y] + P_HEADROOM ? mx - P_HEADROOM : m[z][y];
+            if (above_limit(mx)) c[z][y] = __uint_as_float(0x7fffffffu);
+            const float to = mx > m[z][y] + P_HEADROOM ? reference_for(mx) : m[z][y];
             const float f = ex2_approx(m[z][y] - to);
             m[z][y] = to;
             l[z][y] *= f;
@@ -383,6 +383,7 @@ __global__ void __launch_bounds__(MERGE_GROUPS * D / 4) packed_merge_rows_kernel
     const float4 v = sh_o[i][c];
     acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
   }
+  sum = final_sum(top, sum);
   const float inv = n == 0 ? 0.f : 1.f / sum;  // (with tokens the sum is positive, or NaN)
   const int token = row / p.group, h = head * p.group + row % p.group;
   *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(token) * (p.c.n_kv * p.group) + h) * D + c * 4) =

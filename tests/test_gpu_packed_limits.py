@@ -1,0 +1,55 @@
+"""GPU: the packed cache at the limits of what its calls take, against the definitions in 64 bits."""
+import pytest
+
+import packed_reference as ref
+from test_gpu_packed import attend, gen, make, per_head, randn
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------- logits far below the others
+
+
+def far_and_near(n_q, n, near, seed):
+    """Two heads of 64.  Every third row looks along element 0, where the tokens outside ``near`` lie at -6144 and those of it at zero: their
+    logits there are -3.1e6 and -6.3e6 (from 2.9e6 on a largest logit is too large in magnitude), those of ``near`` ordinary."""
+    import torch
+    g = gen(seed)
+    k, v, q = randn(g, n, 2, 64), randn(g, n, 2, 64), randn(g, n_q, 2, 64)
+    far = torch.ones(n, dtype=torch.bool, device="cuda")
+    far[near] = False
+    k[:, :, 0] = torch.where(far, -6144.0, 0.0).bfloat16()[:, None]
+    looks = torch.arange(n_q, device="cuda") % 3 == 0
+    q[:, :, 0] = 0.0
+    q[looks, :, 0] = torch.where(torch.arange(n_q, device="cuda")[looks] % 2 == 0, 4096.0, 8192.0).bfloat16()[:, None]
+    return q, k, v, looks
+
+
+@pytest.mark.parametrize("n_q", [2, 8, 16, 150, 700])
+@pytest.mark.parametrize("n,near", [(700, slice(699, 700)), (700, slice(0, 1)), (700, slice(300, 340)), (20000, slice(19872, 20000)), (20000, slice(9000, 9100)),
+                                    (20000, slice(0, 20000, 1009)), (128, slice(17, 18)), (129, slice(128, 129))])
+def test_a_row_is_as_large_as_its_largest_logit(n_q, n, near):
+    """Tokens far below weigh nothing, wherever they stand and however the work is dealt; the row is that of the others."""
+    q, k, v, looks = far_and_near(n_q, n, near, n)
+    out, lse = attend(make(2, 2, 64, n, k, v), q)
+    hk, hv = per_head(k), per_head(v)
+    ref.check_attend(out[looks], lse[:, looks], q[looks], [x[near] for x in hk], [x[near] for x in hv])
+    ref.check_attend(out[~looks], lse[:, ~looks], q[~looks], hk, hv)
+
+
+@pytest.mark.parametrize("n_q", [2, 16, 150, 700])
+@pytest.mark.parametrize("n", [100, 20000])
+def test_a_row_whose_logits_all_are_far_below_is_nan(n_q, n):
+    """Whether its logits are numbers or beyond them, and no other row; so is one with a single logit far above."""
+    import torch
+    for first in (4096.0, 8192.0, 2.0 ** 60, 2.0 ** 126):
+        q, k, v, looks = far_and_near(n_q, n, slice(0, 0), n)
+        q[0, 0], q[0, 0, 0] = 0.0, first
+        out, lse = attend(make(2, 2, 64, n, k, v), q)
+        assert torch.isnan(out[looks].float()).all() and torch.isnan(lse[:, looks]).all()
+        ref.check_attend(out[~looks], lse[:, ~looks], q[~looks], per_head(k), per_head(v))
+    q, k, v, looks = far_and_near(n_q, n, slice(0, n), n)
+    k[n - 1, :, 0] = 6144.0
+    out, lse = attend(make(2, 2, 64, n, k, v), q)
+    assert torch.isnan(out[looks].float()).all() and torch.isnan(lse[:, looks]).all()
+    ref.check_attend(out[~looks], lse[:, ~looks], q[~looks], per_head(k), per_head(v))
