@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
         top = max(top & 0xffffu, top >> 16);
         float f, back;
         row_factor(__uint_as_float(top << 16), f, back);
-        c = p.scale_log2e * back;
+        c = logit_factor(p.scale_log2e, back);
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
           const uint32_t raw[4] = {v[k].x, v[k].y, v[k].z, v[k].w};

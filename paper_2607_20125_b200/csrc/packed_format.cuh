@@ -147,6 +147,13 @@ __device__ __forceinline__ void row_factor(float amax, float& to_f16, float& bac
   back = (amax < INFINITY) ? 1.f / to_f16 : __uint_as_float(0x7fffffffu);
 }
 
+// From products of such a row to logits in the log2 domain.  The largest rows at the largest scales pass what fp32 holds: a product that is not
+// zero is beyond the limit with the largest factor too (it is 2^-44 at least), and one that is zero stays zero.
+__device__ __forceinline__ float logit_factor(float scale_log2e, float back) {
+  const float c = scale_log2e * back;
+  return c > 3e38f ? 3e38f : c;
+}
+
 // A line of `total` steps is cut into n equal shares: CTA b owns [share_begin(b), share_begin(b + 1)).
 __host__ __device__ inline int64_t share_begin(int64_t b, int64_t total, int64_t n) { return b * total / n; }
 __host__ __device__ inline int share_owner(int64_t step, int64_t total, int64_t n) { return static_cast<int>(((step + 1) * n - 1) / total); }

@@ -85,7 +85,7 @@ __device__ __forceinline__ void stage_row(uint2* qs, float* row_scale, const __n
     const int e = lane * PER + 2 * i, quarter = e / (D / 4), w = e % (D / 4), kk = w / 4, hi = (w / 2) & 1;
     words[((kk * 2 + (r >> 3)) * 32 + (r & 7) * 4 + quarter) * 2 + hi] = pack_f16x2(x[2 * i] * f, x[2 * i + 1] * f);
   }
-  if (lane == 0) row_scale[r] = scale_log2e * back;
+  if (lane == 0) row_scale[r] = logit_factor(scale_log2e, back);
 }
 
 // NQ: tiles of eight query rows

@@ -53,3 +53,23 @@ def test_a_row_whose_logits_all_are_far_below_is_nan(n_q, n):
     out, lse = attend(make(2, 2, 64, n, k, v), q)
     assert torch.isnan(out[looks].float()).all() and torch.isnan(lse[:, looks]).all()
     ref.check_attend(out[~looks], lse[:, ~looks], q[~looks], per_head(k), per_head(v))
+
+
+@pytest.mark.parametrize("n_q", [2, 16, 150])
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_of_zero_whatever_the_row_and_the_scale(n_q, d):
+    """A row of 2^112 that meets only zeros, at the largest scale: its logits are zero, though row times scale is more than fp32 holds."""
+    import torch
+    g = gen(n_q + d)
+    n, scale = 700, 2.0 ** 40
+    k, v, q = randn(g, n, 2, d), randn(g, n, 2, d), randn(g, n_q, 2, d, scale=1 / scale)
+    k[:, :, 0] = q[:, :, 0] = 0.0
+    q[::2] = 0.0
+    q[::2, :, 0] = 2.0 ** 112
+    cache = make(2, 2, d, n, k, v, softmax_scale=scale)
+    hk, hv = per_head(k), per_head(v)
+    out, lse = attend(cache, q)
+    ref.check_attend(out, lse, q, hk, hv, scale)
+    cache.observe(q, lse, decay=0.0)
+    for (w, err), got in zip(ref.observe(q, lse, hk, scale), cache.weights.double()):
+        assert ((got - w).abs() <= err + 2.0 ** -21 * w).all()
