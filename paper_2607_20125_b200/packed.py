@@ -164,6 +164,8 @@ class PackedCache:
         self.n_heads, self.head_dim, self.capacity = n_heads, head_dim, capacity
         self.n_kv_heads = n_heads if n_kv_heads is None else n_kv_heads
         self.cfg = PackedConfig(_int(n_heads, "n_heads"), _int(self.n_kv_heads, "n_kv_heads"), _int(head_dim, "head_dim"), _int(capacity, "capacity"), softmax_scale)
+        if softmax_scale != 0.0 and self.cfg.softmax_scale == 0.0:  # ctypes cut it down to the zero that selects the default
+            raise ValueError(f"softmax_scale: {softmax_scale} is out of range")
         size = self.lib.headcast_packed_bytes(C.byref(self.cfg))
         if size < 0:
             raise HeadCastError(size, "sizes out of range (1..64 heads, a divisor of them for keys and values, head_dim 64 or 128, capacity 1..2^23, "
