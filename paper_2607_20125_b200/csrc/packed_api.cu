@@ -8,7 +8,6 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
-#include <limits>
 #include <new>
 #include <type_traits>
 
@@ -20,6 +19,7 @@
 #include "packed_rows_kernel.cuh"
 #include "rope_kernel.cuh"
 #include "tmap.h"
+#include "turns.h"
 
 using namespace hc;
 
@@ -219,18 +219,6 @@ int attend_many(headcast_packed* c, const void* q, void* out, float* lse, int32_
   return HC_OK;
 }
 
-// floor(x 2^64) for 0 < x < 1, from the 64-bit significand and the exponent of an extended number (with 64 conversions by casts, each
-// of which changes the rounding mode, a small rotation's call took the host 10.2 us instead of 4.8).
-uint64_t fraction_bits(long double x) {
-  static_assert(std::numeric_limits<long double>::digits == 64, "x86 extended precision");
-  uint64_t significand;
-  uint16_t exponent;
-  std::memcpy(&significand, &x, 8);
-  std::memcpy(&exponent, reinterpret_cast<const char*>(&x) + 8, 2);
-  const int shift = 16382 - exponent;  // x = significand 2^(exponent - 16383 - 63)
-  return shift < 64 ? significand >> shift : 0;
-}
-
 thread_local char g_rope_error[256] = "";
 
 int rope_fail(int code, const char* msg) {
@@ -308,19 +296,13 @@ int headcast_rope(const headcast_rope_config* cfg, const void* q, void* q_out, i
   const int dims[3] = {cfg->dim_t, cfg->dim_h, cfg->dim_w};
   const double scales[3] = {cfg->scale_t, cfg->scale_h, cfg->scale_w};
   for (int a = 0, i = 0; a < 3; ++a) {
-    // One power per axis: 31 products in 64 bits of mantissa lose 2^-59, and a power takes 100 ns, of which 64 were half of a small call.
-    const long double ratio = dims[a] ? powl(static_cast<long double>(cfg->theta), -2.0L / dims[a]) : 1.0L;
-    long double turns = static_cast<long double>(scales[a]) / 6.283185307179586476925286766559L;
-    for (int j = 0; j < dims[a] / 2; ++j, ++i, turns *= ratio) {
-      uint64_t f = 0;
-      if (turns > 0.0L && turns < 1.0L) {
-        f = fraction_bits(turns);
-      } else {
-        if (!std::isfinite(static_cast<double>(turns))) return rope_fail(HC_ERR_INVALID_ARG, "a frequency is not finite");
-        const long double fraction = turns - floorl(turns);  // whole turns per position change nothing
-        if (fraction < 1.0L - 0x1p-64L) f = static_cast<uint64_t>(fraction * 0x1p64L);
-      }
-      p.frequency[i] = inverse ? 0 - f : f;
+    // One root per axis; the j-th product is off by (2 + 4 j) 2^-64 of itself.
+    const Extended ratio = dims[a] > 2 ? inverse_root(cfg->theta, dims[a] / 2) : Extended{};
+    Extended turns = product(extended(std::fabs(scales[a])), TURNS_PER_RADIAN);
+    for (int j = 0; j < dims[a] / 2; ++j, ++i, turns = product(turns, ratio)) {
+      if (turns.e > 1024) return rope_fail(HC_ERR_INVALID_ARG, "a frequency is not finite");
+      const uint64_t f = fraction_of_turn(turns);  // whole turns per position change nothing
+      p.frequency[i] = (scales[a] < 0.0) != (inverse != 0) ? 0 - f : f;
     }
   }
   // Tokens of a block (their sines and cosines are formed once for all heads): 4 where every SM gets a few blocks (three frames of 45 x 80,

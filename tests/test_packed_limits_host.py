@@ -1,7 +1,16 @@
 """The packed cache's and the rotation's host code at the limits of what its calls take.  No GPU."""
+import ctypes as C
+import decimal
+import functools
+import os
+import subprocess
+import tempfile
+
 import pytest
 
 from paper_2607_20125_b200 import packed
+
+NATIVE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "native")
 
 
 @pytest.mark.parametrize("scale", [1e-60, -1e-60, 2.0 ** -151, 5e-324])
@@ -14,3 +23,64 @@ def test_a_scale_that_a_c_float_cannot_hold_is_not_taken_for_the_default(scale):
 def test_scales_out_of_range_are_refused(scale):
     with pytest.raises(packed.HeadCastError, match="softmax_scale"):
         packed.PackedCache(4, 64, 100, softmax_scale=scale)
+
+
+# ---------------------------------------------------------------------------------------------- a rotation's frequencies
+
+
+@functools.lru_cache(maxsize=None)
+def rotation(*flags):
+    """packed_api.cu on the CUDA runtime made for tests, and what its rotation hands to the kernel."""
+    path = os.path.join(tempfile.mkdtemp(), "rope_fake.so")
+    cmd = [os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-cudart", "none", "-shared", "-Xcompiler", ",".join(("-fPIC", "-fno-gnu-unique") + flags), "-Xlinker", "-Bsymbolic",
+           "-gencode", "arch=compute_100a,code=sm_100a", "-Xptxas", "-O0", "-std=c++17", "-o", path,
+           os.path.join(NATIVE, "rope_on_fake_cuda.cu"), os.path.join(NATIVE, "fake_cuda.cpp")]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stdout + res.stderr
+    lib = C.CDLL(path)
+    real = packed.load_library()
+    for name in ("headcast_rope_default_config", "headcast_rope", "headcast_rope_last_error"):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = getattr(real, name).argtypes, getattr(real, name).restype
+    lib.fake_frequencies.argtypes, lib.fake_frequencies.restype = [C.POINTER(C.c_uint64)], C.c_int
+    return lib
+
+
+def frequencies(lib, dims, theta, scales, inverse=0, n=4):
+    cfg = packed.RopeConfig()
+    lib.headcast_rope_default_config(C.byref(cfg))
+    cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, cfg.grid_h, cfg.grid_w, cfg.theta = 2, 2, 128, 2, 2, theta
+    cfg.dim_t, cfg.dim_h, cfg.dim_w = dims
+    cfg.scale_t, cfg.scale_h, cfg.scale_w = scales
+    buffer = C.create_string_buffer(4096 + 512 * n)
+    rc = lib.headcast_rope(C.byref(cfg), C.addressof(buffer) & ~15, (C.addressof(buffer) + 2048 + 256 * n) & ~15, 0, None, None, 0, n, 0, None, inverse, None)
+    assert rc == 0, lib.headcast_rope_last_error()
+    out = (C.c_uint64 * 64)()
+    assert lib.fake_frequencies(out) == sum(dims) // 2
+    return out[: sum(dims) // 2]
+
+
+CONFIGURATIONS = [((44, 42, 42), 1e4, (1.0, 1.0, 1.0)), ((44, 42, 42), 500.0, (0.25, 1.0, 3.7)), ((128, 0, 0), 1e6, (1.0, 1.0, 1.0)), ((2, 4, 6), 256.0, (1.0, -1.0, -0.3)),
+                  ((64, 32, 32), 1.0, (1.0, 6.2831853, 100.0)), ((42, 42, 44), 0.1, (1.0, 0.0, -7.0)), ((2, 62, 64), 1.0000001, (1e-3, 1e-9, 12.5)),
+                  ((44, 42, 42), 1e300, (1.0, 1e-300, 1e18)), ((4, 8, 16), 1e-12, (1e-3, 1.0, 1.0)), ((10, 20, 30), 3.0000000000000004, (1.0, 1.0, 1.0)), ((8, 0, 8), 65536.0, (0.5, 1.0, 2.0 ** -40))]
+
+
+@pytest.mark.parametrize("flags", [(), ("-mlong-double-64",)], ids=["", "64-bit long double"])
+@pytest.mark.parametrize("dims,theta,scales", CONFIGURATIONS)
+def test_frequencies_are_those_of_exact_arithmetic(flags, dims, theta, scales):
+    """On a host whatever its long double is.  In units of u = 2^-64, relative: the constant and the first product are rounded (1 u each); theta r^n is
+    off by n u (a power's error doubles with a square, which adds u), the root by an n-th of that, and by 2 u where its correction is cut to whole units;
+    every product adds u.  The j-th frequency is off by (2 + 4 j) u of itself, and by less than 2^-64 turns where it is cut."""
+    lib = rotation(*flags)
+    got = frequencies(lib, dims, theta, scales)
+    with decimal.localcontext() as ctx:
+        ctx.prec = 80
+        pi, i = decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798"), 0
+        for width, scale in zip(dims, scales):
+            for j in range(width // 2):
+                turns = decimal.Decimal(scale) / (2 * pi) * decimal.Decimal(theta) ** (decimal.Decimal(-2 * j) / width)
+                off = (got[i] - turns * 2 ** 64) % (1 << 64)
+                bound = (2 + 4 * j) * abs(turns) * decimal.Decimal("1.001") + 1
+                assert min(off, (1 << 64) - off) <= bound, (width, scale, j, turns, off)
+                i += 1
+    back = frequencies(lib, dims, theta, scales, inverse=1)
+    assert all((a + b) % (1 << 64) == 0 for a, b in zip(got, back))
