@@ -316,7 +316,9 @@ const char* headcast_rope_last_error(void);
  *
  * The caller owns all device memory: the cache's storage, and a workspace per call, which no two calls whose GPU work may overlap
  * (other streams, graph replays) may share.  Calls allocate nothing and return without waiting (headcast_packed_check
- * excepted); all but that one may be captured, a replay does what the captured call did: to the lengths that the cache had then.  Calls
+ * excepted); all but that one may be captured, a replay does what the captured call did: to the lengths that the cache had then.  A
+ * workspace or an output overlaps neither a cache's storage, nor another argument of the call unless that is allowed below, and an
+ * input of a call that writes to a cache does not overlap that cache's storage: such calls are refused.  Calls
  * that change a cache are ordered by the caller against its others where they are on different streams.  The device on which a
  * cache was created has to be current.  One cache is used by one host thread at a time. */
 #define HEADCAST_PACKED_MAX_TOKENS 8388608

@@ -26,6 +26,7 @@ using namespace hc;
 struct headcast_packed {
   headcast_packed_config cfg;
   PackedView view;
+  int64_t bytes = 0;  // of the storage, from view.status on
   int device = 0, n_sm = 0;
   float scale = 0.f;
   int32_t len[PACK_MAX_HEADS] = {};
@@ -78,6 +79,8 @@ int64_t layout(const headcast_packed_config& cfg, int64_t (&at)[5]) {
   }
   return total;
 }
+
+bool in_storage(const headcast_packed* c, const void* p, int64_t bytes) { return overlap(c->view.status, c->bytes, p, bytes); }
 
 // A call's cache and device: HC_OK, or the reason in the cache.
 int enter(headcast_packed* c) {
@@ -352,6 +355,7 @@ int headcast_packed_create(const headcast_packed_config* cfg, void* storage, int
     return rc;
   }
   c->cfg = *cfg;
+  c->bytes = layout(*cfg, at);
   c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt(static_cast<float>(cfg->head_dim));
   uint8_t* base = static_cast<uint8_t*>(storage);
   c->view.status = reinterpret_cast<int32_t*>(base);
@@ -413,6 +417,8 @@ int headcast_packed_append(headcast_packed* c, const void* k, const void* v, int
   for (int h = 0; h < c->cfg.n_kv_heads; ++h)
     if (n_tokens > c->cfg.capacity - c->len[h])
       return fail(c, HC_ERR_STATE, "head %d holds %d tokens of at most %d: no room for %d more", h, c->len[h], c->cfg.capacity, n_tokens);
+  const int64_t bytes = 2 * (stride * (n_tokens - 1) + row);
+  if (in_storage(c, k, bytes) || in_storage(c, v, bytes)) return fail(c, HC_ERR_INVALID_ARG, "k or v overlaps the cache's storage");
   PackParams p;
   std::memset(&p, 0, sizeof(p));
   p.c = c->view;
@@ -434,6 +440,9 @@ int headcast_packed_export(headcast_packed* c, int32_t first, int32_t n_tokens, 
   if (first < 0 || n_tokens < 0 || first > c->cfg.capacity - n_tokens) return fail(c, HC_ERR_INVALID_ARG, "tokens out of range");
   if ((k_out && !aligned(k_out)) || (v_out && !aligned(v_out))) return fail(c, HC_ERR_INVALID_ARG, "outputs must be 16-byte aligned device pointers");
   if (n_tokens == 0 || (!k_out && !v_out)) return HC_OK;
+  const int64_t bytes = 2ll * c->cfg.n_kv_heads * n_tokens * c->cfg.head_dim;
+  if ((k_out && in_storage(c, k_out, bytes)) || (v_out && in_storage(c, v_out, bytes)) || (k_out && v_out && overlap(k_out, bytes, v_out, bytes)))
+    return fail(c, HC_ERR_INVALID_ARG, "an output overlaps the cache's storage or the other output");
   UnpackParams p;
   std::memset(&p, 0, sizeof(p));
   p.c = c->view;
@@ -465,8 +474,13 @@ int headcast_packed_attend(headcast_packed* c, const void* q, void* out, float* 
   if (lse && !aligned(lse, 4)) return fail(c, HC_ERR_INVALID_ARG, "lse must be 4-byte aligned");
   const int64_t lse_bytes = 4ll * n_queries * c->cfg.n_heads;
   if (lse && (overlap(lse, lse_bytes, q, q_bytes) || overlap(lse, lse_bytes, out, q_bytes))) return fail(c, HC_ERR_INVALID_ARG, "lse overlaps q or out");
-  if (!aligned(workspace, 256) || workspace_bytes < headcast_packed_workspace_bytes(c, n_queries))
+  const int64_t needed = headcast_packed_workspace_bytes(c, n_queries);
+  if (!aligned(workspace, 256) || workspace_bytes < needed)
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_workspace_bytes(%d)", n_queries);
+  if (in_storage(c, out, q_bytes) || (lse && in_storage(c, lse, lse_bytes)) || in_storage(c, workspace, needed))
+    return fail(c, HC_ERR_INVALID_ARG, "out, lse or the workspace overlaps the cache's storage");
+  if (overlap(workspace, needed, q, q_bytes) || overlap(workspace, needed, out, q_bytes) || (lse && overlap(workspace, needed, lse, lse_bytes)))
+    return fail(c, HC_ERR_INVALID_ARG, "the workspace overlaps q, out or lse");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (few_rows(c, n_queries))
     return c->cfg.head_dim == 128 ? attend_few<128>(c, q, out, lse, n_queries, workspace, st) : attend_few<64>(c, q, out, lse, n_queries, workspace, st);
@@ -494,8 +508,13 @@ int headcast_packed_observe(headcast_packed* c, const void* q, const float* lse,
   }
   if (!aligned(q)) return fail(c, HC_ERR_INVALID_ARG, "q must be a 16-byte aligned device pointer");
   if (!aligned(lse, 4)) return fail(c, HC_ERR_INVALID_ARG, "lse must be a 4-byte aligned device pointer");
-  if (!aligned(workspace, 256) || workspace_bytes < headcast_packed_workspace_bytes(c, n_queries))
+  const int64_t needed = headcast_packed_workspace_bytes(c, n_queries);
+  if (!aligned(workspace, 256) || workspace_bytes < needed)
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_workspace_bytes(%d)", n_queries);
+  const int64_t q_bytes = 2ll * n_queries * c->cfg.n_heads * c->cfg.head_dim, lse_bytes = 4ll * n_queries * c->cfg.n_heads;
+  if (in_storage(c, q, q_bytes) || in_storage(c, lse, lse_bytes) || in_storage(c, workspace, needed))
+    return fail(c, HC_ERR_INVALID_ARG, "q, lse or the workspace overlaps the cache's storage");
+  if (overlap(workspace, needed, q, q_bytes) || overlap(workspace, needed, lse, lse_bytes)) return fail(c, HC_ERR_INVALID_ARG, "the workspace overlaps q or lse");
   if (few_rows(c, n_queries)) {
     PackedObserveRowsParams r;
     std::memset(&r, 0, sizeof(r));
@@ -552,8 +571,7 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
   if (!to || to == c || !keep_host) return fail(c, HC_ERR_INVALID_ARG, "another cache and a number of tokens per head are needed");
   if (to->cfg.n_kv_heads != n_kv || to->cfg.head_dim != d || to->device != c->device)
     return fail(c, HC_ERR_INVALID_ARG, "the other cache has other key/value heads, another head_dim or another device");
-  int64_t at[5];
-  if (overlap(c->view.status, layout(c->cfg, at), to->view.status, layout(to->cfg, at))) return fail(c, HC_ERR_INVALID_ARG, "the caches share storage");
+  if (in_storage(c, to->view.status, to->bytes)) return fail(c, HC_ERR_INVALID_ARG, "the caches share storage");
   if (n_first < 0 || n_recent < 0) return fail(c, HC_ERR_INVALID_ARG, "n_first and n_recent must not be negative");
   SelectParams s;
   std::memset(&s, 0, sizeof(s));
@@ -571,6 +589,9 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_evict_workspace_bytes()");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (most > 0) {
+    const void* places = index ? index : workspace;
+    const int64_t bytes = index ? 4 * (static_cast<int64_t>(index_stride) * (n_kv - 1) + most) : headcast_packed_evict_workspace_bytes(c);
+    if (in_storage(c, places, bytes) || in_storage(to, places, bytes)) return fail(c, HC_ERR_INVALID_ARG, "the index or the workspace overlaps a cache's storage");
     s.weights = c->view.weights;
     s.index = index ? index : static_cast<int32_t*>(workspace);
     s.index_stride = index ? index_stride : c->view.cap;

@@ -9,6 +9,7 @@ import tempfile
 import pytest
 
 from paper_2607_20125_b200 import packed
+from test_packed_host import INVALID, PTR, Cache, launches
 
 NATIVE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "native")
 
@@ -23,6 +24,47 @@ def test_a_scale_that_a_c_float_cannot_hold_is_not_taken_for_the_default(scale):
 def test_scales_out_of_range_are_refused(scale):
     with pytest.raises(packed.HeadCastError, match="softmax_scale"):
         packed.PackedCache(4, 64, 100, softmax_scale=scale)
+
+
+# ---------------------------------------------------------------------------------------------- arguments that overlap
+
+
+def test_arguments_that_overlap_each_other_or_a_cache():
+    c, other = Cache(), Cache()
+    assert c.append(PTR, PTR, 50, 0, None) == 0
+    lib, size = c.lib, c.lib.headcast_packed_bytes(C.byref(c.cfg))
+    end = c.at + size
+    arena = C.create_string_buffer(c.workspace_bytes(8) + (1 << 20))
+    q = (C.addressof(arena) + 255) & ~255
+    q_bytes, lse_bytes, ws = 8 * 4 * 64 * 2, 8 * 4 * 4, c.workspace_bytes(8)
+    out, lse, at = q + 65536, q + 131072, q + 262144
+    keep = (C.c_int32 * 2)(5, 5)
+    packed_row = 2 * 64 * 2  # one token's keys, or values
+    launches()
+    for call in (lambda: c.append(c.at, PTR, 1, 0, None), lambda: c.append(PTR, end - 16, 1, 0, None), lambda: c.append(PTR, (c.at - packed_row + 16), 1, 0, None),
+                 lambda: c.append(c.at - 2 * (3 * 256 + 128) + 16, PTR, 4, 256, None),
+                 lambda: c.export(0, 5, c.at, None, None), lambda: c.export(0, 5, None, end - 16, None), lambda: c.export(0, 5, q, q + 5 * packed_row - 16, None),
+                 lambda: c.export(0, 5, q, q, None),
+                 lambda: c.attend(q, end - 16, None, 8, at, ws, None), lambda: c.attend(q, out, C.c_void_p(c.at + 256), 8, at, ws, None),
+                 lambda: c.attend(q, out, None, 8, c.at, ws, None), lambda: c.attend(q, out, None, 8, q, ws, None), lambda: c.attend(q, out, None, 8, out, ws, None),
+                 lambda: c.attend(at + ws - 16, out, None, 8, at, ws, None), lambda: c.attend(q, at + ws - 16, None, 8, at, ws, None),
+                 lambda: c.attend(q, out, C.c_void_p(at + ws - 4), 8, at, ws, None), lambda: c.attend(q, out, C.c_void_p(at - lse_bytes + 4), 8, at, ws, None),
+                 lambda: c.observe(c.at + 256, lse, 8, 1.0, at, ws, None), lambda: c.observe(q, end - 4, 8, 1.0, at, ws, None), lambda: c.observe(q, lse, 8, 1.0, c.at, ws, None),
+                 lambda: c.observe(at + ws - 16, lse, 8, 1.0, at, ws, None), lambda: c.observe(q, at + ws - 4, 8, 1.0, at, ws, None),
+                 lambda: c.evict(other.ptr, keep, 0, 0, c.at, 5, None, 0, None), lambda: c.evict(other.ptr, keep, 0, 0, other.at + size - 4, 5, None, 0, None),
+                 lambda: c.evict(other.ptr, keep, 0, 0, other.at - 36, 5, None, 0, None), lambda: c.evict(other.ptr, keep, 0, 0, None, 0, other.at, 1 << 20, None),
+                 lambda: c.evict(other.ptr, keep, 0, 0, None, 0, c.at, 1 << 20, None)):
+        assert call() == INVALID and "overlaps" in c.error(), c.error()
+    assert launches() == [] and c.lens() == [50, 50] and other.lens() == [0, 0]
+    # side by side
+    for call in (lambda: c.append(PTR, end, 1, 0, None), lambda: c.append(c.at - packed_row, PTR, 1, 0, None), lambda: c.export(0, 5, q, q + 5 * 2 * packed_row // 2, None),
+                 lambda: c.attend(at - q_bytes, at + ws, C.c_void_p(at + ws + q_bytes), 8, at, ws + 4096, None),  # a larger workspace is touched as far as it is needed
+                 lambda: c.attend(q, q, None, 8, at, ws, None), lambda: c.attend(c.at + 256, out, None, 8, at, ws, None),  # reads its cache, writes elsewhere
+                 lambda: c.observe(at + ws, at - lse_bytes, 8, 1.0, at, ws, None), lambda: c.evict(other.ptr, keep, 0, 0, other.at - 40, 5, None, 0, None),
+                 lambda: c.evict(other.ptr, keep, 0, 0, other.at + size, 5, None, 0, None)):
+        assert call() == 0, c.error()
+    none = (C.c_int32 * 2)(0, 0)
+    assert c.evict(other.ptr, none, 0, 0, other.at, 0, None, 0, None) == 0  # writes no index
 
 
 # ---------------------------------------------------------------------------------------------- a rotation's frequencies
