@@ -255,7 +255,7 @@ int headcast_rope(const headcast_rope_config* cfg, const void* q, void* q_out, i
   if (cfg->halves && width % 16 != 0) return rope_fail(HC_ERR_UNSUPPORTED, "halves need a rotated width that is a multiple of 16");
   if (!(cfg->theta > 0.0 && std::isfinite(cfg->theta)) || !std::isfinite(cfg->scale_t) || !std::isfinite(cfg->scale_h) || !std::isfinite(cfg->scale_w))
     return rope_fail(HC_ERR_INVALID_ARG, "theta must be positive, theta and the scales finite");
-  if (!positions && (cfg->grid_h < 1 || cfg->grid_w < 1 || static_cast<int64_t>(cfg->grid_h) * cfg->grid_w > INT32_MAX))
+  if (n_tokens > 0 && !positions && (cfg->grid_h < 1 || cfg->grid_w < 1 || static_cast<int64_t>(cfg->grid_h) * cfg->grid_w > INT32_MAX))
     return rope_fail(HC_ERR_INVALID_ARG, "without positions the grid must be given");
   if (n_tokens < 0) return rope_fail(HC_ERR_INVALID_ARG, "n_tokens must not be negative");
   if (first_frame < -(int64_t(1) << 31) || first_frame > (int64_t(1) << 31)) return rope_fail(HC_ERR_INVALID_ARG, "first_frame out of range");
@@ -585,7 +585,7 @@ int headcast_packed_evict(headcast_packed* c, headcast_packed* to, const int32_t
     most = std::max(most, s.keep.n[h]);
   }
   if (index && (!aligned(index, 4) || index_stride < most)) return fail(c, HC_ERR_INVALID_ARG, "index must be 4-byte aligned with rows of at least %d", most);
-  if (!index && (!aligned(workspace, 256) || workspace_bytes < headcast_packed_evict_workspace_bytes(c)))
+  if (most > 0 && !index && (!aligned(workspace, 256) || workspace_bytes < headcast_packed_evict_workspace_bytes(c)))
     return fail(c, HC_ERR_INVALID_ARG, "the workspace must be 256-byte aligned and hold headcast_packed_evict_workspace_bytes()");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (most > 0) {

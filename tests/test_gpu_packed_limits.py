@@ -73,3 +73,24 @@ def test_logits_of_zero_whatever_the_row_and_the_scale(n_q, d):
     cache.observe(q, lse, decay=0.0)
     for (w, err), got in zip(ref.observe(q, lse, hk, scale), cache.weights.double()):
         assert ((got - w).abs() <= err + 2.0 ** -21 * w).all()
+
+
+# ---------------------------------------------------------------------------------------------- nothing to do
+
+
+def test_calls_with_empty_tensors():
+    import torch
+    from paper_2607_20125_b200.packed import Rope
+    g = gen(50)
+    cache, other = make(4, 2, 64, 50, randn(g, 30, 2, 64), randn(g, 30, 2, 64)), make(4, 2, 64, 50, randn(g, 7, 2, 64), randn(g, 7, 2, 64))
+    q = randn(g, 5, 4, 64)
+    rope = Rope(4, 64, dims=(24, 20, 20))  # no grid: positions are given
+    rope.apply(q[:0], q[:0], positions=torch.zeros(0, 3, dtype=torch.int32, device="cuda"))
+    cache.append(randn(g, 0, 2, 64), randn(g, 0, 2, 64))
+    cache.attend(q[:0], q[:0], torch.empty(4, 0, device="cuda"))
+    cache.observe(q[:0], torch.empty(4, 0, device="cuda"))
+    assert cache.export(first=3, n_tokens=0)[0].shape == (2, 0, 64) and cache.lengths() == [30, 30]
+    cache.evict_into(other, 0, index=torch.empty(2, 0, dtype=torch.int32, device="cuda"))
+    assert other.lengths() == [0, 0] and other.export()[0].shape == (2, 0, 64) and other.weights.shape == (2, 0)
+    other.evict_into(cache, 9, index=torch.empty(2, 0, dtype=torch.int32, device="cuda"))
+    assert cache.lengths() == [0, 0]

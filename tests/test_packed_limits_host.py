@@ -126,3 +126,26 @@ def test_frequencies_are_those_of_exact_arithmetic(flags, dims, theta, scales):
                 i += 1
     back = frequencies(lib, dims, theta, scales, inverse=1)
     assert all((a + b) % (1 << 64) == 0 for a, b in zip(got, back))
+
+
+# ---------------------------------------------------------------------------------------------- nothing to do
+
+
+def test_calls_without_tokens_need_no_addresses():
+    """The address of an empty tensor is null."""
+    lib = packed.load_library()
+    cfg = packed.RopeConfig()
+    lib.headcast_rope_default_config(C.byref(cfg))
+    cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, cfg.dim_t = 2, 2, 64, 64  # no grid: positions are given
+    assert lib.headcast_rope(C.byref(cfg), None, None, 0, None, None, 0, 0, 0, None, 0, None) == 0
+    assert lib.headcast_rope(C.byref(cfg), PTR, PTR, 0, None, None, 0, 1, 0, None, 0, None) == INVALID and b"grid" in lib.headcast_rope_last_error()
+    c, other = Cache(), Cache()
+    assert other.append(PTR, PTR, 7, 0, None) == 0
+    none = (C.c_int32 * 2)(0, 0)
+    launches()
+    for keep in (none, (C.c_int32 * 2)(9, 9)):  # the cache is empty
+        assert c.evict(other.ptr, keep, 0, 0, None, 0, None, 0, None) == 0 and other.lens() == [0, 0], c.error()
+        assert other.append(PTR, PTR, 7, 0, None) == 0
+    assert other.evict(c.ptr, none, 0, 0, None, 0, None, 0, None) == 0 and c.lens() == [0, 0] and other.lens() == [7, 7]
+    assert other.evict(c.ptr, (C.c_int32 * 2)(0, 1), 0, 0, None, 0, None, 0, None) == INVALID and "workspace" in other.error()
+    assert "evict_select_kernel" not in launches()
