@@ -2,7 +2,7 @@
 import pytest
 
 import packed_reference as ref
-from test_gpu_packed import attend, gen, make, per_head, randn
+from test_gpu_packed import attend, check_evict, gen, make, per_head, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -73,6 +73,32 @@ def test_logits_of_zero_whatever_the_row_and_the_scale(n_q, d):
     cache.observe(q, lse, decay=0.0)
     for (w, err), got in zip(ref.observe(q, lse, hk, scale), cache.weights.double()):
         assert ((got - w).abs() <= err + 2.0 ** -21 * w).all()
+
+
+# ---------------------------------------------------------------------------------------------- lengths around what eviction keeps in registers
+
+
+@pytest.mark.parametrize("n", [98303, 98304, 98305])
+def test_eviction_at_the_border_of_what_registers_hold(n):
+    """Twelve keys for each of 1024 threads of eight blocks."""
+    import torch
+    g = gen(n)
+    cache = make(1, 1, 64, n, randn(g, n, 1, 64), randn(g, n, 1, 64))
+    cache.weights.copy_(torch.randint(0, 5000, (1, n), device="cuda", generator=g).float())
+    check_evict(cache, [n // 3], 10, 1000)
+    check_evict(cache, [n - 1], 0, 0)
+
+
+def test_eviction_of_heads_on_both_sides_of_that_border():
+    import torch
+    g = gen(40)
+    n, kv = 98400, 4
+    source = make(kv, kv, 64, n, randn(g, n, kv, 64), randn(g, n, kv, 64))
+    cache = make(kv, kv, 64, n)
+    source.evict_into(cache, [98304, 98305, 500, 0], n_first=n)
+    cache.weights.copy_(torch.randint(0, 5000, (kv, 98305), device="cuda", generator=g).float())
+    check_evict(cache, [30000, 30001, 77, 5], 3, 100)
+    check_evict(cache, [98304, 98304, 499, 0], 0, 0)
 
 
 # ---------------------------------------------------------------------------------------------- nothing to do
