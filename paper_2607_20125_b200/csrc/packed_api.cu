@@ -311,7 +311,7 @@ int headcast_rope(const headcast_rope_config* cfg, const void* q, void* q_out, i
   // Tokens of a block (their sines and cosines are formed once for all heads): 4 where every SM gets a few blocks (three frames of 45 x 80,
   // pairs side by side, 27.8 us and of 68 x 120 56.6; 8 tokens 32.3 and 58.1, 16 tokens 37.6 and 67), fewer in small calls.
   int per_block = 4;
-  while (per_block > 1 && (n_tokens + per_block - 1) / per_block < 148 * 4) per_block /= 2;
+  while (per_block > 1 && (n_tokens + per_block - 1) / per_block < ROPE_MANY_BLOCKS) per_block /= 2;
   const dim3 grid((n_tokens + per_block - 1) / per_block);
   const size_t smem = static_cast<size_t>(per_block) * (d / 2) * sizeof(float2);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

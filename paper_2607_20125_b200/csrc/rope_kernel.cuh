@@ -25,6 +25,7 @@ struct RopeParams {
   uint64_t frequency[ROPE_MAX_PAIRS];  // in 2^-64 turns per position; negated for the inverse
 };
 constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_MANY_BLOCKS = 4 * 148;  // four for each SM of a B200: a value for tuning alone, any number of blocks gives the same results
 
 // HALVES: pairs are (i, i + pairs) instead of (2i, 2i + 1).
 // TOKENS per block: a power of two that leaves enough blocks (chosen by the caller).
