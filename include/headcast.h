@@ -365,7 +365,8 @@ int64_t headcast_packed_workspace_bytes(const headcast_packed* cache, int32_t n_
  * [n_heads][n_queries] float, the natural logarithm of the sum of the exponentials.  A head without tokens gives zeros and -infinity; a
  * query row that holds a NaN or an infinity, or whose largest logit (the greatest over its tokens) is 2.9e6 or more in magnitude, gives
  * NaN in both outputs; tokens whose logits are further below count for nothing.
- * Probabilities enter the second product in fp16, sums are fp32.  The result does not depend on anything but the inputs and
+ * A query row enters the first product in fp16 relative to a power of two of its own: exact but for elements below 2^-28 of its largest,
+ * which are off by up to 2^-39 of that.  Probabilities enter the second product in fp16, sums are fp32.  The result does not depend on anything but the inputs and
  * the GPU's number of SMs. */
 int headcast_packed_attend(headcast_packed* cache, const void* q_dev, void* out_dev, float* lse_dev, int32_t n_queries, void* workspace_dev,
                            int64_t workspace_bytes, void* stream);

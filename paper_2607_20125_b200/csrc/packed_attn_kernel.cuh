@@ -16,8 +16,9 @@
 // The packed streams are 3.6 times smaller than bf16, so they share L2 where bf16 streams had to be taken in turn.
 //
 // What bounds it: a tile's softmax (1700 clk alone on its schedulers, 2000 beside the other tile's) and its products (1024, and 350 until
-// their results are seen) follow one another; two tiles overlap to 3700 clk a step.  4680 queries x 32760 tokens, 12 heads of 128: 730 us,
-// 1290 TFLOP/s, and at the power cap up to 850; 10800 x 75600: 4.35 ms.
+// their results are seen) follow one another; two tiles overlap to 3700 clk a step.  4680 queries x 32760 tokens, 12 heads of 128: 740 us,
+// 1270 TFLOP/s, and 850 for seconds on end, at the power cap; 10800 x 75600: 4.37 ms.  At d = 64, 16 heads, 4680 x 32760 take 917 us, 2.4 times
+// their products: what bounds them there is not known.  (Stores to spilled registers: 40 bytes a thread at d = 128, 88 at d = 64.)
 #pragma once
 #include "packed_format.cuh"
 
@@ -101,7 +102,7 @@ __global__ void __launch_bounds__(PATTN_THREADS, 1) packed_attn_kernel(const __g
   using SM = PackedAttnSmem<D>;
   constexpr int QK_STEPS = D / 16;
   // Pairs of exponentials whose index has these bits set take the polynomial: an eighth at d = 128 (a quarter 746 us for a 30 x 52 block, an
-  // eighth 729, a sixteenth 727), a quarter at d = 64, where the products take half the time (935 us, 970, 980 for 16 heads).
+  // eighth 729, a sixteenth 727: the last two are level), a quarter at d = 64, where the products take half the time (935 us, 970, 980 for 16 heads).
   constexpr int POLY = D == 128 ? 7 : 3;
   constexpr uint32_t TMEM_COLS = 512;
   constexpr uint32_t S_COL = 0, O_COL = 256;  // S_t at t*128, O_t at 256 + t*128; P_t overlays the first half of S_t

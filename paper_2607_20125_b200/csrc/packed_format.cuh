@@ -112,7 +112,7 @@ __device__ __forceinline__ uint32_t pack_word(const uint32_t (&raw)[4], uint32_t
 // ---- what the attention kernels share
 
 // The first multiple of ALIGN in a block's dynamic shared memory, as an offset from it: an address rounded as an integer is a generic
-// one to the compiler, and every access through it takes the path of global memory (converting a tile: 1300 clk instead of 500).
+// one to the compiler, and every access through it takes the path of global memory (converting a tile: 1300 clk instead of 850).
 template <uint32_t ALIGN>
 __device__ __forceinline__ uint8_t* aligned_shared(uint8_t* raw) {
   return raw + ((ALIGN - smem_u32(raw) % ALIGN) % ALIGN);
@@ -122,8 +122,8 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
                : "memory");
 }
-// Probabilities are formed relative to a reference 6 below the maximum that set it and are at most 2^14: fp16 holds them down
-// to 2^-24, 2^-30 of the largest.
+// Probabilities are formed relative to a reference 6 below the maximum that set it and are at most 2^14 (packed_attn_kernel bounds a tile's sum
+// of them instead, by P_MOST): fp16 holds them down to 2^-24, 2^-30 of the largest.
 constexpr float P_HEADROOM = 6.f, P_LAG = 14.f;
 // The reference of a row that has met no logit yet (or only NaNs): below all of them, and finite, so that exponentials need no case for it.
 constexpr float NO_REFERENCE = -3e38f;

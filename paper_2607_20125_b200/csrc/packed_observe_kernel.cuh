@@ -9,9 +9,10 @@
 //   warp 0 issues products, warp 1 loads query tiles, warps 2 and 3 their log-sum-exps, warps 4-7 convert the next pair of
 //   tiles while this one is in use, warps 8-23 add up: four per scheduler, since with two (a thread per token) the loop waited for its own
 //   latencies, 3300 clk a step.
-// What bounds it: one exponential per logit, 2 * 128 * 128 per step, 2048 clk of the special-function unit beside 1024 clk of
-// products; a quarter of the exponentials is therefore evaluated on the FMA pipe (none to a half of them: level to 20 % slower).  A step
-// takes 2700 clk: the pipes of four warps per scheduler do not overlap fully.  4680 queries x 32760 tokens, 12 heads of 128: 528 us.
+// What bounds it: latency.  One exponential per logit, 2 * 128 * 128 per step, would be 2048 clk of the special-function unit beside 1024 clk of
+// products; a quarter of the exponentials is evaluated on the FMA pipe (none to a half of them: level to 20 % slower).  A step takes 2700 clk,
+// the unit busy 57 % of them: a warp waits for each of its loads from tensor memory right behind its issue.  4680 queries x 32760 tokens,
+// 12 heads of 128: 543 us, and 620 for seconds on end, at the power cap.
 #pragma once
 #include "packed_attn_kernel.cuh"
 
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(POBS_THREADS, 1) packed_observe_kernel(const _
       mbar_arrive_if(&bar_k_full[kb], lane == 0);
     }
   } else {
-    // ------------------------------------------------------------------ sums: one thread per token
+    // ------------------------------------------------------------------ sums: two threads per token, half of a tile's columns each
     const int t = ((warp - 8) >> 2) & 1, r = ((warp & 3) << 5) | lane, half = (warp - 8) >> 3;
     const uint32_t s_addr = tmem + (static_cast<uint32_t>((warp & 3) << 5) << 16) + t * 128 + half * 64;
     const uint64_t c2 = pack_f32x2(p.scale_log2e, p.scale_log2e);

@@ -14,8 +14,8 @@
 //   - the maximum is only looked for, across lanes, when some logit outgrows the reference;
 //   - operands are fp16: held values are exact in it, query rows are brought to a common power of two first (see row_factor), and
 //     probabilities keep 11 bits.  tcgen05 products want 128 rows, eight times the conversions' share here.
-// One query, 12 heads of 128: 18.1 us for 32760 tokens (3.1 TB/s), 52 for 131072 (4.3 TB/s).  Turning codes into operands bounds it, the
-// integer pipe is the busiest; 8 us of the first are launches, first loads and the merge.
+// One query, 12 heads of 128: 18.1 us for 32760 tokens (3.1 TB/s), 52 for 131072 (4.3 TB/s).  Latency bounds it, between the loads of a tile, their
+// conversion and the products: the integer pipe, the busiest, is at 51 %, memory at 45 %.  8 us of the first are launches, first loads and the merge.
 #pragma once
 #include "packed_format.cuh"
 
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(MERGE_GROUPS * D / 4) packed_merge_rows_kernel
 // The products are those of packed_rows_kernel without the values; a row of S^T is a token and its columns the queries, so a
 // token's sum is four lanes' to add and each token belongs to one warp: no parts, no second kernel.  Keys are read straight into registers, a
 // tile ahead; 80 bytes per token and head at d = 128.  One query, 32760 tokens, 12 heads of 128: 9.1 us (3.4 TB/s;
-// packed_observe_kernel, for which one query is as much work as 32: 32); 131072 tokens 29.5 (4.3).  Conversions bound it.
+// packed_observe_kernel, for which one query is as much work as 32: 32); 131072 tokens 29.5 (4.3).  Bound like packed_rows_kernel.
 struct PackedObserveRowsParams {
   PackedView c;
   const __nv_bfloat16* q;
